@@ -55,7 +55,7 @@ typedef enum {
 } mbp_status;
 
 typedef enum { MBP_HEAD_LCA = 0, MBP_HEAD_MLP = 1 } mbp_head;
-typedef enum { MBP_F32 = 0, MBP_BF16 = 1, MBP_F16 = 2 } mbp_dtype;
+typedef enum { MBP_F32 = 0, MBP_BF16 = 1, MBP_F16 = 2, MBP_MXFP4 = 3 /* caches only */ } mbp_dtype;
 typedef enum { MBP_ACCEPT_THRESHOLD = 0, MBP_ACCEPT_SELF_VERIFY = 1 } mbp_mode;
 
 /* Model architecture and capacities.
@@ -340,6 +340,120 @@ void mbp_destroy(mbp_handle *h);
 
 /* Last error message of the handle ("" if none); valid until the next call. */
 const char *mbp_last_error(const mbp_handle *h);
+
+/* ------------------------------------------------------------------------------------
+ * Paged caches: keys and values of many sequences in pages, and the operators on them.
+ *
+ * These calls need no handle.  They allocate nothing, wait for nothing, keep no state and
+ * may be captured into a graph; all device work goes to the stream given, which must be of
+ * the current device, as must every device pointer.  Several threads may call them at
+ * once.  They return an mbp_status; arguments are checked before any device work, and
+ * mbp_paged_error() says what was wrong.  What lies in device memory (page ids, row
+ * starts, slots, ranges, positions) cannot be checked here: the kernels bound every access
+ * by the sizes given, so that a bad value costs that row's result and no more.
+ */
+
+/* A cache.
+ *   dtype       MBP_BF16 or MBP_F16: values in 16 bits; finite values beyond float16's
+ *               largest are held as that.  MBP_MXFP4: e2m1 codes in 4 bits with one scale
+ *               2^(byte - 127) for each 32 consecutive channels of a slot and head
+ *               (4.25 bits a value); the scale's exponent is floor(log2 of the block's
+ *               largest magnitude) - 2, within [-127, 127], codes are the nearest (ties
+ *               to the even code) and saturate at 6; a block with a NaN or an infinity
+ *               gets byte 255 and reads as NaN.
+ *   n_kv_heads, d_head   heads and channels (32, 64 or 128).
+ *   page_size   slots of a page: a power of two, 16 to 1024.
+ *   n_pages     pages of each pool.
+ *   n_seqs, max_pages   the page table's rows and columns; max_pages x page_size <= 2^30.
+ *   d_k, d_v    pools, each [n_pages][n_kv_heads] pages of one head, aligned to 16 bytes:
+ *               [page_size][d_head] 16-bit values, or [page_size][d_head / 2] bytes of
+ *               codes (channel 2j in the low half of byte j) followed by
+ *               [page_size][d_head / 32] scale bytes.
+ *   d_pages     int32 [n_seqs][max_pages]: slot s of sequence i is slot s % page_size of
+ *               page d_pages[i][s / page_size].  An id outside [0, n_pages) means that
+ *               there is no page: what is appended there is dropped, and no row sees it.
+ *               Sequences may share pages that no call appends to. */
+typedef struct {
+  int32_t dtype, n_kv_heads, d_head, page_size, n_pages, n_seqs, max_pages;
+  void *d_k, *d_v;
+  const int32_t *d_pages;
+} mbp_paged_cache;
+
+/* The token rows of one call: rows d_row_start[i] .. d_row_start[i+1] - 1 are sequence
+ * i's, in slots d_first_slot[i] onwards (sequences may have no rows).  Rows before the
+ * first or behind the last sequence's belong to none.
+ *   n_rows      rows of the arrays given with it.
+ *   max_rows    at least the most rows of one sequence: attention leaves the rows behind
+ *               a sequence's first max_rows as they were.
+ *   max_slots   about the most slots that a row sees: attention divides its work by it
+ *               (a wrong value costs time, not results).
+ *   d_row_start int32 [n_seqs + 1], ascending;  d_first_slot int32 [n_seqs]. */
+typedef struct {
+  int32_t n_rows, max_rows, max_slots;
+  const int32_t *d_row_start;
+  const int32_t *d_first_slot;
+} mbp_paged_rows;
+
+/* [n_rows][heads][d_head] values of MBP_F32, MBP_BF16 or MBP_F16: channel c of head h of
+ * row r at d + r row_stride + h head_stride + c (elements).  Strides are at least 0; those
+ * of outputs keep all heads apart.  Any alignment to the element; heads that all start at
+ * multiples of 16 bytes are faster. */
+typedef struct {
+  void *d;
+  int32_t dtype;
+  int64_t row_stride, head_stride;
+} mbp_paged_heads;
+
+/* What the last failed call of this thread on paged caches objected to ("" if none). */
+const char *mbp_paged_error(void);
+
+/* Bytes of each pool (0 for an invalid shape; pointers are not looked at). */
+size_t mbp_paged_pool_bytes(const mbp_paged_cache *cache);
+
+/* Table of rotations, float [n_pos][d_head / 2][2]: cosine and sine of
+ * p base^(-2j / d_head), aligned to 16 bytes. */
+int mbp_rope_table(float *d_table, int32_t n_pos, int32_t d_head, float base, void *hip_stream);
+
+/* Append token rows: keys are rotated and, like the values, stored in their slots; with
+ * queries, those are rotated into q_out.
+ *   q, q_out    n_heads heads each (a multiple of n_kv_heads), of one dtype; both NULL for
+ *               none (n_heads is not read then).  q_out may be q itself.
+ *   k, v        n_kv_heads heads.
+ *   d_pos       int32 [n_rows] rotary positions, or NULL: the rows' slots.
+ *   d_rope      table of n_pos positions as mbp_rope_table makes it, or NULL: no rotation
+ *               (channels 2j and 2j + 1 become x0 cos - x1 sin and x0 sin + x1 cos).
+ * A row of no sequence, or whose position is not in the table, is left out: nothing of it
+ * is written.  A row whose slot has no page gets its q_out and is not stored. */
+int mbp_paged_append(const mbp_paged_cache *cache, const mbp_paged_rows *rows, int32_t n_heads,
+                     const mbp_paged_heads *q, const mbp_paged_heads *q_out, const mbp_paged_heads *k,
+                     const mbp_paged_heads *v, const int32_t *d_pos, const float *d_rope, int32_t n_pos,
+                     void *hip_stream);
+
+/* Read rows back: all n_rows of k_out and v_out are written with the values in their
+ * slots, 0 for a row of no sequence or a slot without a page (in float16, finite values
+ * beyond the largest become that). */
+int mbp_paged_read(const mbp_paged_cache *cache, const mbp_paged_rows *rows, const mbp_paged_heads *k_out,
+                   const mbp_paged_heads *v_out, void *hip_stream);
+
+/* Bytes of the workspace that mbp_paged_attend needs for these shapes and bounds (the
+ * pointers in them are not looked at); often 0, and 0 for invalid ones. */
+size_t mbp_paged_workspace_bytes(const mbp_paged_cache *cache, const mbp_paged_rows *rows, int32_t n_heads);
+
+/* Attention of token rows over their sequences' slots:
+ *   out[r][h] = sum over s of softmax_s(scale q[r][h] . k[s][h / (n_heads / n_kv_heads)]) v[s][..]
+ * over the slots lo <= s < hi that have a page; 0 for a row that sees none.
+ *   q, out      n_heads heads (a multiple of n_kv_heads), of one dtype: MBP_F32, the
+ *               cache's own 16-bit dtype, or either over MBP_MXFP4.
+ *   d_lo, d_hi  int32 [n_rows]: the slots that each row sees, for causal, document, group,
+ *               prefix and window masks alike.  NULL: from slot 0; up to the row's own.
+ *   scale       finite, 1 / sqrt(d_head) as a rule.
+ *   d_work      device workspace of work_bytes >= mbp_paged_workspace_bytes, aligned to 16
+ *               bytes, contents of no matter; used until the call's work has finished.
+ * Scores, softmax and sums are float32.  What slots hold that a row does not see, be it
+ * NaN, does not reach it.  The same call gives the same bits. */
+int mbp_paged_attend(const mbp_paged_cache *cache, const mbp_paged_rows *rows, int32_t n_heads,
+                     const mbp_paged_heads *q, const mbp_paged_heads *out, const int32_t *d_lo, const int32_t *d_hi,
+                     float scale, void *d_work, size_t work_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

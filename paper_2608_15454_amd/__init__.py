@@ -11,15 +11,20 @@ import os
 
 import numpy as np
 
+from .paged import PagedCache, PagedRows, rope_table
+from .paged import declare as _declare_paged
+
 __all__ = [
     "MbpConfig", "MbpError", "Decoder", "lib", "lib_path", "make_config", "weight_manifest",
     "HEAD_LCA", "HEAD_MLP", "F32", "BF16", "F16", "THRESHOLD", "SELF_VERIFY",
     "OK", "EINVAL", "ECAPACITY", "EHIP", "ESTATE",
+    "MXFP4", "PagedCache", "PagedRows", "rope_table",
 ]
 
 OK, EINVAL, ECAPACITY, EHIP, ESTATE = 0, -1, -2, -3, -4
 HEAD_LCA, HEAD_MLP = 0, 1
 F32, BF16, F16 = 0, 1, 2
+MXFP4 = 3  # caches only
 THRESHOLD, SELF_VERIFY = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -115,6 +120,7 @@ def lib():
     L.mbp_set_timing.restype = ctypes.c_int
     L.mbp_read_timing.argtypes = [P, ctypes.POINTER(KernelTime)]
     L.mbp_read_timing.restype = ctypes.c_int
+    _declare_paged(L)
     _lib = L
     return L
 

@@ -1,0 +1,1131 @@
+// Paged cache operators for gfx950: token rows into pages of 16-bit or MXFP4 values with
+// the position rotation applied on the way, the way back, and attention over the pages.
+#include "paged.h"
+
+#include <hip/hip_ext.h>
+
+#include <algorithm>
+
+#include "dev.h"
+
+namespace mbp {
+using namespace dev;
+namespace {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename Kern, typename... Args>
+hipError_t plaunch(Kern kernel, dim3 grid, dim3 block, hipStream_t st, hipEvent_t e0, hipEvent_t e1, Args... args) {
+  if (e0 != nullptr || e1 != nullptr) hipExtLaunchKernelGGL(kernel, grid, block, 0, st, e0, e1, 0, args...);
+  else hipLaunchKernelGGL(kernel, grid, block, 0, st, args...);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------- rows and elements ----
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const f32x2_t v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const f32x2_t v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+
+__device__ __forceinline__ float lo_bf16(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float hi_bf16(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ float lo_f16(uint32_t u) { return (float)__builtin_bit_cast(f16x2, u)[0]; }
+__device__ __forceinline__ float hi_f16(uint32_t u) { return (float)__builtin_bit_cast(f16x2, u)[1]; }
+
+// Elements [at, at + 8) of rows of type t.
+__device__ __forceinline__ void load8(const void* p, int64_t at, int t, int vec, float (&x)[8]) {
+  if (t == PT_F32) {
+    const float* f = reinterpret_cast<const float*>(p) + at;
+    if (vec) {
+      const float4 a = *reinterpret_cast<const float4*>(f), b = *reinterpret_cast<const float4*>(f + 4);
+      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+      x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = f[i];
+    }
+    return;
+  }
+  const uint16_t* h = reinterpret_cast<const uint16_t*>(p) + at;
+  uint32_t u[4];
+  if (vec) {
+    const uint4 a = *reinterpret_cast<const uint4*>(h);
+    u[0] = a.x; u[1] = a.y; u[2] = a.z; u[3] = a.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = (uint32_t)h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = t == PT_BF16 ? lo_bf16(u[i]) : lo_f16(u[i]);
+    x[2 * i + 1] = t == PT_BF16 ? hi_bf16(u[i]) : hi_f16(u[i]);
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void store_n(void* p, int64_t at, int t, int vec, const float (&x)[N]) {
+  if (t == PT_F32) {
+    float* f = reinterpret_cast<float*>(p) + at;
+    if (vec && N % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i + 3 < N; i += 4) *reinterpret_cast<float4*>(f + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) f[i] = x[i];
+    }
+    return;
+  }
+  uint16_t* h = reinterpret_cast<uint16_t*>(p) + at;
+  uint32_t u[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) u[i] = t == PT_BF16 ? pack_bf16(x[2 * i], x[2 * i + 1]) : pack_f16(x[2 * i], x[2 * i + 1]);
+  if (vec && N % 8 == 0) {
+#pragma unroll
+    for (int i = 0; i + 3 < N / 2; i += 4) *reinterpret_cast<uint4*>(h + 2 * i) = make_uint4(u[i], u[i + 1], u[i + 2], u[i + 3]);
+  } else if (vec && N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i + 1 < N / 2; i += 2) *reinterpret_cast<uint2*>(h + 2 * i) = make_uint2(u[i], u[i + 1]);
+  } else if (vec) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) *reinterpret_cast<uint32_t*>(h + 2 * i) = u[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      h[2 * i] = (uint16_t)u[i];
+      h[2 * i + 1] = (uint16_t)(u[i] >> 16);
+    }
+  }
+}
+
+// The rows of sequence s, whatever row_start holds: [row0, row0 + n) within [0, n_rows).
+struct SeqRows {
+  int32_t row0, n, slot0;
+};
+__device__ __forceinline__ SeqRows seq_rows(const PagedRows& r, int s) {
+  const int32_t a = min(max(r.row_start[s], 0), r.n_rows), b = min(max(r.row_start[s + 1], a), r.n_rows);
+  return {a, b - a, r.first_slot[s]};
+}
+
+// The sequence that holds row `row`, or -1: the last one that begins at or before it.  A
+// wave looks through 64 starts at a time; row is the same in all its lanes.
+__device__ __forceinline__ int seq_of(const PagedRows& r, int n_seqs, int row) {
+  const int lane = threadIdx.x & 63;
+  int s = -1;
+  for (int at = 0; at < n_seqs; at += 64) {
+    const int i = at + lane;
+    s += (int)__popcll(__ballot(i < n_seqs && r.row_start[min(i, n_seqs)] <= row));
+  }
+  return s;
+}
+
+// Byte offset of slot 0 of a page of head h, or -1 where the slot has no page.
+__device__ __forceinline__ int64_t page_of(const PagedCache& c, int s, int32_t slot, int h) {
+  if (slot < 0 || (slot >> c.shift) >= c.max_pages) return -1;
+  const int32_t id = c.pages[(int64_t)s * c.max_pages + (slot >> c.shift)];
+  if ((uint32_t)id >= (uint32_t)c.n_pages) return -1;
+  return ((int64_t)id * c.hk + h) * c.page_bytes;
+}
+
+// Largest of four neighbouring lanes' values.
+__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kDppXor2, 0xF, 0xF, false));
+  return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kDppXor1, 0xF, 0xF, false));
+}
+
+// Scale exponent e of a block of 32 values from the largest biased exponent among them:
+// floor(log2 amax) - 2, which puts amax into [4, 8) steps of the largest e2m1 binade.
+// Returns 255 for a block with a NaN or an infinity.
+__device__ __forceinline__ int scale_byte(int exponent, int special) {
+  return exponent >= special ? 255 : min(max(exponent - special / 2 - 2, -127), 127) + 127;
+}
+
+// Codes of 8 values y (already divided by the scale), nearest-even, saturated at 6.
+__device__ __forceinline__ uint32_t codes8(const float (&y)[8]) {
+  uint32_t u = 0;
+  u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[0], y[1], 1.0f, 0);
+  u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[2], y[3], 1.0f, 1);
+  u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[4], y[5], 1.0f, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[6], y[7], 1.0f, 3);
+}
+
+// d as float32 whose last bit says whether something was cut off (round to odd): rounding
+// that again to fewer bits gives what rounding d would give.
+__device__ __forceinline__ float round_odd(double d) {
+  const float f = (float)d;
+  uint32_t u = __float_as_uint(f);
+  const double back = (double)f;
+  if (back != d) {
+    if (fabs(back) > fabs(d)) u -= 1;
+    u |= 1;
+  }
+  return __uint_as_float(u);
+}
+
+// ------------------------------------------------------------------- append ----
+// A thread takes 8 channels of one head of one row, the heads of a row in the order q, k,
+// v; 4 neighbouring threads share a scale block of 32.  Every value is read once and
+// written once, so the copy rate bounds it; the rotation is three operations a channel.
+template <int CT>
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, int units_row, int64_t units) {
+  const int64_t u0 = (int64_t)blockIdx.x * 256;
+  const int row0 = (int)(u0 / units_row);
+  int s = seq_of(a.r, a.c.n_seqs, row0);
+  // units past the block's first row: the quotient is small, float32 has it exactly but
+  // for the last unit, which the comparisons put right
+  int unit = (int)(u0 - (int64_t)row0 * units_row) + threadIdx.x;
+  int off = (int)((float)unit / (float)units_row);
+  off += unit - off * units_row >= units_row;
+  off -= unit - off * units_row < 0;
+  unit -= off * units_row;
+  const int row = row0 + off;
+  if (u0 + threadIdx.x >= units) return;
+  while (s + 1 < a.c.n_seqs && a.r.row_start[s + 1] <= row) ++s;
+  if (s < 0) return;
+  const SeqRows sr = seq_rows(a.r, s);
+  if (row < sr.row0 || row >= sr.row0 + sr.n) return;
+  const int32_t slot = (int32_t)min((int64_t)sr.slot0 + (row - sr.row0), (int64_t)INT32_MAX);
+  const int dh = a.c.dh, per = dh >> 3;
+  const int nq = a.q.p != nullptr ? a.H : 0;
+  int h = unit / per;
+  const int c0 = (unit - h * per) * 8;
+  const int which = h < nq ? 0 : h < nq + a.c.hk ? 1 : 2;
+  h -= which == 0 ? 0 : which == 1 ? nq : nq + a.c.hk;
+  float x[8];
+  const HeadRows& src = which == 0 ? a.q : which == 1 ? a.k : a.v;
+  float4 cs[4];
+  const bool turn = which < 2 && a.rope != nullptr;
+  if (turn) {
+    const int32_t pos = a.pos != nullptr ? a.pos[row] : slot;
+    if ((uint32_t)pos >= (uint32_t)a.n_pos) return;
+    const float4* t = reinterpret_cast<const float4*>(a.rope + ((int64_t)pos * dh + c0) / 2);
+    cs[0] = t[0];
+    cs[1] = t[1];
+  } else if (a.rope != nullptr && a.pos != nullptr) {
+    if ((uint32_t)a.pos[row] >= (uint32_t)a.n_pos) return;
+  } else if (a.rope != nullptr && (uint32_t)slot >= (uint32_t)a.n_pos) {
+    return;
+  }
+  load8(src.p, (int64_t)row * src.row + (int64_t)h * src.head + c0, src.type, src.vec, x);
+  if (which == 0 || CT != PT_MXFP4) {
+    if (turn) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float c = i & 1 ? cs[i >> 1].z : cs[i >> 1].x, sn = i & 1 ? cs[i >> 1].w : cs[i >> 1].y;
+        const float r0 = x[2 * i] * c - x[2 * i + 1] * sn, r1 = x[2 * i] * sn + x[2 * i + 1] * c;
+        x[2 * i] = r0;
+        x[2 * i + 1] = r1;
+      }
+    }
+    if (which == 0) {
+      store_n(a.qo.p, (int64_t)row * a.qo.row + (int64_t)h * a.qo.head + c0, a.qo.type, a.qo.vec, x);
+      return;
+    }
+  }
+  const int64_t page = page_of(a.c, s, slot, h);
+  if (page < 0) return;
+  char* pool = (which == 1 ? a.c.k : a.c.v) + page;
+  const int at = slot & ((1 << a.c.shift) - 1);
+  if constexpr (CT != PT_MXFP4) {
+    if constexpr (CT == PT_F16) {  // finite values beyond the type's largest are held as that
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = fabsf(x[i]) < INFINITY ? fminf(fmaxf(x[i], -65504.f), 65504.f) : x[i];
+    }
+    store_n(pool, (int64_t)at * dh + c0, CT, 1, x);
+  } else {
+    // A value beside the middle of two codes has to go to the right one, and so has the
+    // largest value beside a power of two: keys are rotated in float64, where the products
+    // are exact, and reach the conversion through a float32 that is rounded to odd.
+    float y[8];
+    int byte;
+    if (turn) {
+      double d[8];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const double c = i & 1 ? cs[i >> 1].z : cs[i >> 1].x, sn = i & 1 ? cs[i >> 1].w : cs[i >> 1].y;
+        d[2 * i] = (double)x[2 * i] * c - (double)x[2 * i + 1] * sn;
+        d[2 * i + 1] = (double)x[2 * i] * sn + (double)x[2 * i + 1] * c;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, (uint32_t)(__builtin_bit_cast(uint64_t, d[i]) >> 32) & 0x7fffffffu);
+      byte = scale_byte((int)(quad_max(top) >> 20), 2047);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = round_odd(ldexp(d[i], 127 - byte));
+    } else {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+      byte = scale_byte((int)(quad_max(top) >> 23), 255);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = ldexpf(x[i], 127 - byte);
+    }
+    const uint32_t u = byte == 255 ? 0u : codes8(y);
+    *reinterpret_cast<uint32_t*>(pool + (at * dh + c0) / 2) = u;
+    if ((c0 & 31) == 0) pool[(dh / 2 << a.c.shift) + at * (dh >> 5) + (c0 >> 5)] = (char)byte;
+  }
+}
+
+// --------------------------------------------------------------------- read ----
+__global__ __launch_bounds__(256) void paged_read_kernel(PagedCache c, PagedRows r, HeadRows ko, HeadRows vo, int units_row,
+                                                         int64_t units) {
+  const int64_t u0 = (int64_t)blockIdx.x * 256;
+  const int row0 = (int)(u0 / units_row);
+  int s = seq_of(r, c.n_seqs, row0);
+  int unit = (int)(u0 - (int64_t)row0 * units_row) + threadIdx.x;
+  int off = (int)((float)unit / (float)units_row);
+  off += unit - off * units_row >= units_row;
+  off -= unit - off * units_row < 0;
+  unit -= off * units_row;
+  const int row = row0 + off;
+  if (u0 + threadIdx.x >= units) return;
+  while (s + 1 < c.n_seqs && r.row_start[s + 1] <= row) ++s;
+  int32_t slot = -1;  // of no sequence: nothing there
+  if (s >= 0) {
+    const SeqRows sr = seq_rows(r, s);
+    if (row >= sr.row0 && row < sr.row0 + sr.n) slot = (int32_t)min((int64_t)sr.slot0 + (row - sr.row0), (int64_t)INT32_MAX);
+  }
+  const int dh = c.dh, per = dh >> 3;
+  int h = unit / per;
+  const int c0 = (unit - h * per) * 8;
+  const bool val = h >= c.hk;
+  h -= val ? c.hk : 0;
+  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const int64_t page = page_of(c, s, slot, h);
+  if (page >= 0) {
+    const char* pool = (val ? c.v : c.k) + page;
+    const int at = slot & ((1 << c.shift) - 1);
+    if (c.type != PT_MXFP4) {
+      load8(pool, (int64_t)at * dh + c0, c.type, 1, x);
+    } else {
+      const uint32_t u = *reinterpret_cast<const uint32_t*>(pool + (at * dh + c0) / 2);
+      const float sc = __uint_as_float((uint32_t)(uint8_t)pool[(dh / 2 << c.shift) + at * (dh >> 5) + (c0 >> 5)] << 23);
+      const bf16x2_t b[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 1),
+                             __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 3)};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = lo_bf16(__builtin_bit_cast(uint32_t, b[i]));
+        x[2 * i + 1] = hi_bf16(__builtin_bit_cast(uint32_t, b[i]));
+      }
+    }
+  }
+  const HeadRows& dst = val ? vo : ko;
+  if (dst.type == PT_F16) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = fabsf(x[i]) < INFINITY ? fminf(fmaxf(x[i], -65504.f), 65504.f) : x[i];
+  }
+  store_n(dst.p, (int64_t)row * dst.row + (int64_t)h * dst.head + c0, dst.type, dst.vec, x);
+}
+
+// ------------------------------------------------------------------- attend ----
+// Products run on 16-bit matrix instructions with float32 sums: float16 for a float16
+// cache, bfloat16 for the others (an e2m1 code times a power of two is a bfloat16 value).
+// Queries and probabilities enter as one to three terms of that type, so that what they
+// lose stays below the rounding of the output: kQ query terms, kP probability terms.
+template <int CT, int QT, int MAXQ = 3>
+struct Terms {
+  static constexpr bool same = QT == CT || (CT == PT_MXFP4 && QT == PT_BF16);
+  // float32 queries: float16 pairs hold 22 bits of a row scaled to its largest value,
+  // bfloat16 triples 24; float16 queries over MXFP4 are exact as bfloat16 pairs
+  static constexpr int kQ = same ? 1 : CT == PT_F16 ? 2 : QT == PT_F16 ? 2 : MAXQ;
+  // probabilities: one term has half a step of the output's own type (of bfloat16 for
+  // MXFP4), two terms 2^-16 to 2^-22
+  static constexpr int kP = QT == PT_F32 ? 2 : same ? 1 : 2;
+};
+
+template <int CT>
+__device__ __forceinline__ uint32_t pack_pair(float a, float b) {
+  if constexpr (CT == PT_F16) return pack_f16(a, b);
+  else return pack_bf16(a, b);
+}
+template <int CT>
+__device__ __forceinline__ float lo_of(uint32_t u) {
+  if constexpr (CT == PT_F16) return lo_f16(u);
+  else return lo_bf16(u);
+}
+template <int CT>
+__device__ __forceinline__ float hi_of(uint32_t u) {
+  if constexpr (CT == PT_F16) return hi_f16(u);
+  else return hi_bf16(u);
+}
+
+// 8 values as N terms of the product's type, each the rounded rest of the ones before.
+template <int CT, int N>
+__device__ __forceinline__ void split8(const float (&x)[8], u32x4 (&t)[N]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = x[2 * i], b = x[2 * i + 1];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const uint32_t u = pack_pair<CT>(a, b);
+      t[n][i] = u;
+      if (n + 1 < N) {
+        a -= lo_of<CT>(u);
+        b -= hi_of<CT>(u);
+      }
+    }
+  }
+}
+
+template <int CT>
+__device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (CT == PT_F16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+template <int CT>
+__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (CT == PT_F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// 8 codes of one scale block as bfloat16.
+__device__ __forceinline__ u32x4 decode8(uint32_t u, uint32_t scale_byte) {
+  const float sc = __uint_as_float(scale_byte << 23);
+  u32x4 r;
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 0));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 1));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 2));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 3));
+  return r;
+}
+
+// The 4 x 16 tile of 16-bit values that the 16 lanes of a quarter wave point at (lane i:
+// four values of row i / 4) turned round: lane i receives the four rows' values of
+// column i.
+__device__ __forceinline__ uint2 read_turned(const uint16_t* p) {
+  return __builtin_bit_cast(
+      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(uintptr_t)lds_addr(p)));
+}
+
+// One element of a cache row.
+template <int CT, int DH>
+__device__ __forceinline__ float cache_at(const char* page, int shift, int at, int c) {
+  if constexpr (CT == PT_BF16) return bf2f(reinterpret_cast<const uint16_t*>(page)[at * DH + c]);
+  if constexpr (CT == PT_F16) return (float)reinterpret_cast<const _Float16*>(page)[at * DH + c];
+  const uint32_t u = (uint8_t)page[(at * DH + c) / 2];
+  const uint32_t s = (uint8_t)page[(DH / 2 << shift) + at * (DH / 32) + c / 32];
+  const bf16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, __uint_as_float(s << 23), 0);
+  return c & 1 ? hi_bf16(__builtin_bit_cast(uint32_t, b)) : lo_bf16(__builtin_bit_cast(uint32_t, b));
+}
+
+// Largest and smallest over 16 neighbouring lanes.
+__device__ __forceinline__ int min16(int x) {
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) x = min(x, __shfl_xor(x, o));
+  return x;
+}
+__device__ __forceinline__ int max16(int x) {
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) x = max(x, __shfl_xor(x, o));
+  return x;
+}
+
+// The value sums of N channels from c0 on, one visible slot after the other.  A matrix
+// product adds 0 times the value of a slot that its row must not see, which is NaN when
+// that value is an infinity or NaN; a row whose sum of probabilities is finite and whose
+// output is not is summed again this way.  Never taken for finite caches.
+template <int CT, int DH, int N>
+__device__ __forceinline__ void sum_values(const PagedAttend& a, int s, int kvh, int row, int head, int lo, int hi, float m,
+                                           float f, int c0, float (&o)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = 0.f;
+#pragma unroll 1
+  for (int slot = lo; slot < hi; ++slot) {
+    const int64_t page = page_of(a.c, s, slot, kvh);
+    if (page < 0) continue;
+    const int at = slot & ((1 << a.c.shift) - 1);
+    float dot = 0.f;
+#pragma unroll 1
+    for (int c = 0; c < DH; c += 8) {
+      float q[8];
+      load8(a.q.p, (int64_t)row * a.q.row + (int64_t)head * a.q.head + c, a.q.type, a.q.vec, q);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dot += q[i] * cache_at<CT, DH>(a.c.k + page, a.c.shift, at, c + i);
+    }
+    const float p = __builtin_amdgcn_exp2f(dot * f - m);
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] += p * cache_at<CT, DH>(a.c.v + page, a.c.shift, at, c0 + i);
+  }
+}
+
+// Slots [lo, hi) that row tok of its sequence sees; lo = cap, hi = 0 for none.
+__device__ __forceinline__ void row_range(const PagedAttend& a, const SeqRows& sr, int tok, int cap, int* lo, int* hi) {
+  const int row = sr.row0 + tok;
+  *lo = a.lo != nullptr ? max(a.lo[row], 0) : 0;
+  *hi = (int)min(a.hi != nullptr ? (int64_t)a.hi[row] : (int64_t)sr.slot0 + tok + 1, (int64_t)cap);
+  if (*lo >= *hi) {
+    *lo = cap;
+    *hi = 0;
+  }
+}
+
+struct Grid {  // of an attention launch, one-dimensional: split fastest, then KV head, tile, sequence
+  int32_t S, chunk, tiles;
+};
+
+// Where a row's channels go: the output, or this split's sums.
+template <int N>
+__device__ __forceinline__ void put_out(const PagedAttend& a, int S, int split, int row, int head, int dh, int c0, float m, float l,
+                                        float (&o)[N]) {
+  if (S == 1) {
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = l == 0.f ? 0.f : o[i] * inv;
+    store_n(a.o.p, (int64_t)row * a.o.row + (int64_t)head * a.o.head + c0, a.o.type, a.o.vec, o);
+    return;
+  }
+  const int64_t i = ((int64_t)split * a.r.n_rows + row) * a.H + head, all = (int64_t)S * a.r.n_rows * a.H;
+  store_n(a.work, i * dh + c0, PT_F32, 1, o);
+  if (c0 == 0) reinterpret_cast<float2*>(a.work + all * dh)[i] = make_float2(m, l);
+}
+
+// Up to 16 query rows of one sequence and KV head (its rows times the query heads of the
+// group, row-major) against the slots of one split.  Four waves take blocks of KT slots in
+// turn and join their softmax states at the end.  Computed transposed, so that lane l
+// owns query l % 16 (16x16x32 products; lane l supplies row or column l % 16 and the 8
+// positions 8 (l / 16).. of the contracted dimension, and receives rows 4 (l / 16).. of
+// column l % 16):
+//   S^T = K Q^T: keys come straight from the pages into the operand registers, a lane
+//     holding DH / 4 consecutive channels of its key (the contraction may run over the
+//     channels in any order, so the queries are held in the same one);
+//   O^T += V^T P^T: the probabilities are already where the product wants them, values
+//     go through the wave's own LDS tile and are read turned round.
+// The next block's loads are in flight during a block's softmax and value product.
+template <int CT, int DH, int QT>
+__global__ __launch_bounds__(256) void paged_step_kernel(PagedAttend a, Grid gr) {
+  using T = Terms<CT, QT>;
+  constexpr bool F4 = CT == PT_MXFP4;
+  constexpr int KT = DH == 128 ? 32 : F4 || DH == 32 ? 64 : 32;
+  constexpr int NB = KT / 16, KS = DH / 32, CB = DH / 16, PITCH = DH + 8;
+  constexpr int VU = F4 ? KT * DH / 32 / 64 : KT * DH / 8 / 64;  // 16-byte pieces of a block's values per lane
+  static_assert(VU >= 1, "a block has a piece for every lane");
+  constexpr int TILE = KT * PITCH * 2, MERGE = 16 * (DH + 4) * 4;
+  __shared__ __attribute__((aligned(16))) char lds[4 * (TILE > MERGE ? TILE : MERGE)];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
+  int bid = blockIdx.x;
+  const int split = bid % gr.S;
+  bid /= gr.S;
+  const int kvh = bid % a.c.hk;
+  bid /= a.c.hk;
+  const int tile = bid % gr.tiles, s = bid / gr.tiles;
+  const int G = a.H / a.c.hk;
+  const SeqRows sr = seq_rows(a.r, s);
+  const int nq = min(sr.n, a.r.max_rows) * G;
+  if (tile * 16 >= nq) return;
+  const int cap = a.c.max_pages << a.c.shift;
+  const int qi = tile * 16 + col, tok = min(qi, nq - 1) / G, head = kvh * G + min(qi, nq - 1) - tok * G, row = sr.row0 + tok;
+  int lo = cap, hi = 0;
+  if (qi < nq) row_range(a, sr, tok, cap, &lo, &hi);
+  const int kmin = __builtin_amdgcn_readfirstlane(min16(lo)), kmax = __builtin_amdgcn_readfirstlane(max16(hi));
+  const int lo_all = __builtin_amdgcn_readfirstlane(max16(hi > 0 ? lo : 0)), hi_all = __builtin_amdgcn_readfirstlane(min16(hi > 0 ? hi : cap));
+  const int64_t b0 = (int64_t)(kmin & ~(KT - 1)) + (int64_t)split * gr.chunk;
+  const int begin = (int)min(b0, (int64_t)cap);
+  const int end = split == gr.S - 1 ? kmax : (int)min((int64_t)kmax, b0 + gr.chunk);
+
+  // queries: channels g DH / 4 + 8 ks .. +7 of row col in step ks
+  float f = a.scale * 1.44269504f;  // probabilities are 2^(f s - f max)
+  float sign = f < 0.f ? -1.f : f == 0.f ? 0.f : 1.f;
+  f = f == 0.f ? 1.f : fabsf(f);
+  u32x4 q[KS][T::kQ];
+  {
+    float x[KS][8];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      load8(a.q.p, (int64_t)row * a.q.row + (int64_t)head * a.q.head + g * (DH / 4) + ks * 8, QT, a.q.vec, x[ks]);
+    }
+    if constexpr (CT == PT_F16 && QT == PT_F32) {  // into the range of float16, by a power of two
+      float top = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[ks][i]));
+      top = across_max<16>(top);
+      const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+      sign = ldexpf(sign, -e);
+      f = ldexpf(f, e);
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[ks][i] *= sign;
+      split8<CT, T::kQ>(x[ks], q[ks]);
+    }
+  }
+
+  f32x4 o[CB];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) o[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+
+  uint16_t* const vt = reinterpret_cast<uint16_t*>(lds + wave * TILE);
+  u32x4 kr[NB][F4 ? 1 : KS], vr[VU];
+  uint32_t ksc[NB], vsc[VU];
+  const int32_t* const ids = a.c.pages + (int64_t)s * a.c.max_pages;
+  const uint32_t in_page = (1u << a.c.shift) - 1;
+  const int sc_off = DH / 2 << a.c.shift;
+  uint32_t valid = 0;  // of the block whose keys are in the registers: a bit for each 16 slots
+  // Loads of the block at slot t.  16 slots never cross a page; slots at and behind kmax
+  // are read from their page where there is one (any content is masked) and from page 0
+  // where not.
+  auto page_at = [&](int t, bool* ok) {
+    const int n = t >> a.c.shift;
+    const int32_t id = ids[min(n, a.c.max_pages - 1)];
+    *ok = t < kmax && (uint32_t)id < (uint32_t)a.c.n_pages;
+    return ((int64_t)(*ok ? id : 0) * a.c.hk + kvh) * a.c.page_bytes;
+  };
+  auto load = [&](int t) {
+    valid = 0;
+    int64_t pg[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      bool ok;
+      pg[b] = page_at(t + 16 * b, &ok);
+      valid |= (uint32_t)ok << b;
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const char* kp = a.c.k + pg[b];
+      const uint32_t at = ((uint32_t)(t + 16 * b) & in_page) + col;
+      if constexpr (F4) {
+        const char* p = kp + at * (DH / 2) + g * (DH / 8);
+        if constexpr (DH == 128) {
+          kr[b][0] = *reinterpret_cast<const u32x4*>(p);
+        } else if constexpr (DH == 64) {
+          const uint2 u = *reinterpret_cast<const uint2*>(p);
+          kr[b][0][0] = u.x;
+          kr[b][0][1] = u.y;
+        } else {
+          kr[b][0][0] = *reinterpret_cast<const uint32_t*>(p);
+        }
+        ksc[b] = (uint8_t)kp[sc_off + at * (DH / 32) + g * DH / 128];
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kr[b][ks] = *reinterpret_cast<const u32x4*>(kp + (at * DH + g * (DH / 4) + ks * 8) * 2);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < VU; ++u) {
+      // pieces of a block in slot order; the slots of piece u lie in the 16 slots b0
+      constexpr int PER = F4 ? DH / 32 : DH / 8, ROWS = 64 / PER;  // pieces of a slot, slots of one u
+      const int key = u * ROWS + lane / PER;
+      int64_t page = pg[(u * ROWS) / 16];
+      if constexpr (ROWS > 16) {
+#pragma unroll
+        for (int b = 1; b < ROWS / 16; ++b) page = key - u * ROWS >= 16 * b ? pg[(u * ROWS) / 16 + b] : page;
+      }
+      const char* vp = a.c.v + page;
+      const uint32_t at = ((uint32_t)(t + (key & ~15)) & in_page) + (key & 15);
+      vr[u] = *reinterpret_cast<const u32x4*>(vp + at * (F4 ? DH / 2 : DH * 2) + (lane % PER) * 16);
+      if constexpr (F4) vsc[u] = (uint8_t)vp[sc_off + at * PER + lane % PER];
+    }
+  };
+  const int step = 4 * KT;
+  int t = begin + wave * KT;
+  if (t < end) load(t);
+  for (; t < end; t += step) {
+    f32x4 sc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      sc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        u32x4 kf;
+        if constexpr (F4) kf = decode8(kr[b][0][ks], ksc[b]);
+        else kf = kr[b][ks];
+#pragma unroll
+        for (int n = 0; n < T::kQ; ++n) sc[b] = mma16<CT>(kf, q[ks][n], sc[b]);
+      }
+    }
+    const uint32_t ok = valid;
+    // values into the tile; those of slots that no row may see as zeros
+    const bool inner = t >= lo_all && t + KT <= hi_all && ok == (1u << NB) - 1;
+#pragma unroll
+    for (int u = 0; u < VU; ++u) {
+      constexpr int PER = F4 ? DH / 32 : DH / 8, ROWS = 64 / PER;
+      const int key = u * ROWS + lane / PER;
+      const bool see = inner || (t + key >= kmin && t + key < kmax && ((ok >> (key >> 4)) & 1));
+      if constexpr (F4) {
+        u32x4* d = reinterpret_cast<u32x4*>(vt + key * PITCH + (lane % PER) * 32);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = see ? decode8(vr[u][i], vsc[u]) : u32x4{0, 0, 0, 0};
+      } else {
+        *reinterpret_cast<u32x4*>(vt + key * PITCH + (lane % PER) * 8) = see ? vr[u] : u32x4{0, 0, 0, 0};
+      }
+    }
+    if (t + step < end) load(t + step);
+    if (!inner) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int slot = t + 16 * b + 4 * g + r;
+          sc[b][r] = slot >= lo && slot < hi && ((ok >> b) & 1) ? sc[b][r] : -INFINITY;
+        }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[b][r]);
+    mx = across_max<16>(mx);
+    const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn * f;
+    const float alpha = __builtin_amdgcn_exp2f(m * f - ref);
+    m = mn;
+    float ls = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        sc[b][r] = __builtin_amdgcn_exp2f(fmaf(sc[b][r], f, -ref));
+        ls += sc[b][r];
+      }
+    l = l * alpha + ls;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) o[cb] *= alpha;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int b = 0; b < NB; b += 2) {
+      const float x[8] = {sc[b][0], sc[b][1], sc[b][2], sc[b][3], sc[b + 1][0], sc[b + 1][1], sc[b + 1][2], sc[b + 1][3]};
+      u32x4 p[T::kP];
+      split8<CT, T::kP>(x, p);
+      const uint16_t* src = vt + (16 * b + 4 * g + (col >> 2)) * PITCH + (col & 3) * 4;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        const uint2 v0 = read_turned(src + cb * 16), v1 = read_turned(src + 16 * PITCH + cb * 16);
+        const u32x4 vf = {v0.x, v0.y, v1.x, v1.y};
+#pragma unroll
+        for (int n = 0; n < T::kP; ++n) o[cb] = mma16<CT>(vf, p[n], o[cb]);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  l = across_sum<16>(l);
+  if (hi == 0) {  // blocks that all other rows see whole were not masked for a row that sees none
+    m = -INFINITY;
+    l = 0.f;
+  }
+  // join the four waves' states: [wave][query][max, sum, -, -, DH channels]
+  __syncthreads();
+  float* const mb = reinterpret_cast<float*>(lds);
+  {
+    float* w = mb + (wave * 16 + col) * (DH + 4);
+    if (g == 0) {
+      w[0] = m == -INFINITY ? m : m * f;  // in units of log 2
+      w[1] = l;
+    }
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) *reinterpret_cast<float4*>(w + 4 + cb * 16 + g * 4) = make_float4(o[cb][0], o[cb][1], o[cb][2], o[cb][3]);
+  }
+  __syncthreads();
+  // thread: query tid / 16, DH / 16 channels
+  constexpr int N = DH / 16;
+  const int qj = tid >> 4, c0 = (tid & 15) * N, q2 = tile * 16 + qj;
+  if (q2 >= nq) return;
+  float mj = -INFINITY, lj = 0.f, oj[N];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mj = fmaxf(mj, mb[(w * 16 + qj) * (DH + 4)]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) oj[i] = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float* p = mb + (w * 16 + qj) * (DH + 4);
+    if (p[0] == -INFINITY && p[1] == 0.f) continue;  // saw nothing
+    const float e = __builtin_amdgcn_exp2f(p[0] - mj);
+    lj += p[1] * e;
+#pragma unroll
+    for (int i = 0; i < N; ++i) oj[i] += p[4 + c0 + i] * e;
+  }
+  const int tok2 = q2 / G, head2 = kvh * G + q2 - tok2 * G;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) odd |= !(fabsf(oj[i]) < INFINITY);
+  if (odd && lj < INFINITY) {
+    int lo2, hi2;
+    row_range(a, sr, tok2, cap, &lo2, &hi2);
+    sum_values<CT, DH>(a, s, kvh, sr.row0 + tok2, head2, max(lo2, begin), min(hi2, end), mj, a.scale * 1.44269504f, c0, oj);
+  }
+  put_out(a, gr.S, split, sr.row0 + tok2, head2, DH, c0, mj, lj, oj);
+}
+
+// Many query rows: 128 per block (32 per wave, lane l owning query l % 32) against the
+// slots of one split, 64 at a time.  The keys and values of the block's 64 slots lie in
+// LDS for all four waves, the next 64 are loaded during the products.  32x32x16 products
+// (lane l supplies row or column l % 32 and the 8 positions 8 (l / 32).. of the
+// contracted dimension, and receives rows 8 (r / 4) + 4 (l / 32) + r % 4 of column l % 32);
+// everything transposed and the values read turned round, as for few rows.
+template <int CT, int DH, int QT>
+__global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Grid gr) {
+  using T = Terms<CT, QT, DH == 128 ? 2 : 3>;
+  constexpr bool F4 = CT == PT_MXFP4;
+  constexpr int KT = 64, KS = DH / 16, CB = DH / 32, PITCH = DH + 8;
+  // pieces of a tile: 16 bytes (16-bit types: 8 channels, codes: 16 channels of 8 bytes)
+  constexpr int PER = F4 ? DH / 16 : DH / 8, PIECES = KT * PER, NP = PIECES < 256 ? 1 : PIECES / 256;
+  __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][KT * PITCH];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
+  int bid = blockIdx.x;
+  const int split = bid % gr.S;
+  bid /= gr.S;
+  const int tile = gr.tiles - 1 - bid % gr.tiles;  // late rows see the most slots: they go first
+  bid /= gr.tiles;
+  const int kvh = bid % a.c.hk, s = bid / a.c.hk;
+  const int G = a.H / a.c.hk;
+  const SeqRows sr = seq_rows(a.r, s);
+  const int nq = min(sr.n, a.r.max_rows) * G;
+  if (tile * 128 >= nq) return;
+  const int cap = a.c.max_pages << a.c.shift;
+  const int qi = tile * 128 + wave * 32 + col, tok = min(qi, nq - 1) / G, head = kvh * G + min(qi, nq - 1) - tok * G, row = sr.row0 + tok;
+  int lo = cap, hi = 0;
+  if (qi < nq) row_range(a, sr, tok, cap, &lo, &hi);
+  // the wave's extent: [wmin, wmax) holds every visible slot, all of [lo_all, hi_all) is
+  // visible to every row that sees anything
+  auto wide = [&](int x, bool largest) {
+    x = largest ? max16(x) : min16(x);
+    const int y = __shfl_xor(x, 16);
+    return __builtin_amdgcn_readfirstlane(largest ? max(x, y) : min(x, y));
+  };
+  const int wmin = wide(lo, false), wmax = wide(hi, true);
+  const int lo_all = wide(hi > 0 ? lo : 0, true), hi_all = wide(hi > 0 ? hi : cap, false);
+  __shared__ int ext[4][2];
+  if (lane == 0) {
+    ext[wave][0] = wmin;
+    ext[wave][1] = wmax;
+  }
+  __syncthreads();
+  const int kmin = __builtin_amdgcn_readfirstlane(min(min(ext[0][0], ext[1][0]), min(ext[2][0], ext[3][0])));
+  const int kmax = __builtin_amdgcn_readfirstlane(max(max(ext[0][1], ext[1][1]), max(ext[2][1], ext[3][1])));
+  const int64_t b0 = (int64_t)(kmin & ~(KT - 1)) + (int64_t)split * gr.chunk;
+  const int begin = (int)min(b0, (int64_t)cap);
+  const int end = split == gr.S - 1 ? kmax : (int)min((int64_t)kmax, b0 + gr.chunk);
+
+  float f = a.scale * 1.44269504f;
+  float sign = f < 0.f ? -1.f : f == 0.f ? 0.f : 1.f;
+  f = f == 0.f ? 1.f : fabsf(f);
+  u32x4 q[KS][T::kQ];
+  if constexpr (CT == PT_F16 && QT == PT_F32) {
+    float top = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      float x[8];
+      load8(a.q.p, (int64_t)row * a.q.row + (int64_t)head * a.q.head + ks * 16 + half * 8, QT, a.q.vec, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+    }
+    top = pair_max<32>(top);
+    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+    sign = ldexpf(sign, -e);
+    f = ldexpf(f, e);
+  }
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    float x[8];
+    load8(a.q.p, (int64_t)row * a.q.row + (int64_t)head * a.q.head + ks * 16 + half * 8, QT, a.q.vec, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= sign;
+    split8<CT, T::kQ>(x, q[ks]);
+  }
+  f32x16 o[CB];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[cb][r] = 0.f;
+  float m = -INFINITY, l = 0.f;
+
+  const int32_t* const ids = a.c.pages + (int64_t)s * a.c.max_pages;
+  const uint32_t in_page = (1u << a.c.shift) - 1;
+  const int sc_off = DH / 2 << a.c.shift;
+  u32x4 kr[NP], vr[NP];  // (codes: two words each)
+  uint32_t ksc[NP], vsc[NP];
+  auto load = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+      const int i = min(u * 256 + tid, PIECES - 1), key = i / PER, part = i % PER, n = (t + key) >> a.c.shift;
+      const int32_t id = ids[min(n, a.c.max_pages - 1)];
+      const bool ok = t + key >= kmin && t + key < kmax && (uint32_t)id < (uint32_t)a.c.n_pages;
+      const int64_t page = ((int64_t)(ok ? id : 0) * a.c.hk + kvh) * a.c.page_bytes;
+      const uint32_t at = (uint32_t)(t + key) & in_page;
+      if constexpr (F4) {
+        const uint2 x = *reinterpret_cast<const uint2*>(a.c.k + page + at * (DH / 2) + part * 8);
+        const uint2 y = *reinterpret_cast<const uint2*>(a.c.v + page + at * (DH / 2) + part * 8);
+        kr[u][0] = x.x; kr[u][1] = x.y;
+        // codes of slots that no row may see: zeros
+        vr[u][0] = ok ? y.x : 0; vr[u][1] = ok ? y.y : 0;
+        ksc[u] = (uint8_t)a.c.k[page + sc_off + at * (DH / 32) + part / 2];
+        vsc[u] = ok ? (uint8_t)a.c.v[page + sc_off + at * (DH / 32) + part / 2] : 127;
+      } else {
+        kr[u] = *reinterpret_cast<const u32x4*>(a.c.k + page + at * (DH * 2) + part * 16);
+        const u32x4 y = *reinterpret_cast<const u32x4*>(a.c.v + page + at * (DH * 2) + part * 16);
+        vr[u] = ok ? y : u32x4{0, 0, 0, 0};
+      }
+    }
+  };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+      const int i = u * 256 + tid, key = i / PER, part = i % PER;
+      if (PIECES < 256 && i >= PIECES) continue;
+      uint16_t* kd = &lds[buf][0][key * PITCH + part * (DH / PER)];
+      uint16_t* vd = &lds[buf][1][key * PITCH + part * (DH / PER)];
+      if constexpr (F4) {
+        reinterpret_cast<u32x4*>(kd)[0] = decode8(kr[u][0], ksc[u]);
+        reinterpret_cast<u32x4*>(kd)[1] = decode8(kr[u][1], ksc[u]);
+        reinterpret_cast<u32x4*>(vd)[0] = decode8(vr[u][0], vsc[u]);
+        reinterpret_cast<u32x4*>(vd)[1] = decode8(vr[u][1], vsc[u]);
+      } else {
+        *reinterpret_cast<u32x4*>(kd) = kr[u];
+        *reinterpret_cast<u32x4*>(vd) = vr[u];
+      }
+    }
+  };
+  if (begin < end) {
+    load(begin);
+    store(0);
+  }
+  int cur = 0;
+  for (int t = begin; t < end; t += KT, cur ^= 1) {
+    __syncthreads();  // the block's tile is complete, the other buffer is free
+    const bool more = t + KT < end;
+    if (more) load(t + KT);
+    if (t < wmax && t + KT > wmin) {
+      const uint16_t* kt = lds[cur][0];
+      const uint16_t* vt = lds[cur][1];
+      f32x16 sc[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[b][r] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + (32 * b + col) * PITCH + ks * 16 + half * 8);
+#pragma unroll
+          for (int n = 0; n < T::kQ; ++n) sc[b] = mma32<CT>(kf, q[ks][n], sc[b]);
+        }
+      }
+      uint32_t ok = 0;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int32_t id = ids[min((t + 16 * b) >> a.c.shift, a.c.max_pages - 1)];
+        ok |= (uint32_t)((uint32_t)id < (uint32_t)a.c.n_pages) << b;
+      }
+      if (t < lo_all || t + KT > hi_all || ok != 15u) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int slot = t + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3);
+            sc[b][r] = slot >= lo && slot < hi && ((ok >> (2 * b + (r >> 3))) & 1) ? sc[b][r] : -INFINITY;
+          }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[b][r]);
+      mx = pair_max<32>(mx);
+      const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn * f;
+      const float alpha = __builtin_amdgcn_exp2f(m * f - ref);
+      m = mn;
+      float ls = 0.f;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sc[b][r] = __builtin_amdgcn_exp2f(fmaf(sc[b][r], f, -ref));
+          ls += sc[b][r];
+        }
+      l = l * alpha + ls;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) o[cb] *= alpha;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          const float x[8] = {sc[b][8 * k2], sc[b][8 * k2 + 1], sc[b][8 * k2 + 2], sc[b][8 * k2 + 3],
+                              sc[b][8 * k2 + 4], sc[b][8 * k2 + 5], sc[b][8 * k2 + 6], sc[b][8 * k2 + 7]};
+          u32x4 p[T::kP];
+          split8<CT, T::kP>(x, p);
+          // lanes of a quarter wave: channels 16 (lane / 16 % 2) .., slots 4 half .. of the 8
+          const uint16_t* src = vt + (32 * b + 16 * k2 + 4 * half + ((lane & 15) >> 2)) * PITCH + (lane & 16) + (lane & 3) * 4;
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) {
+            const uint2 v0 = read_turned(src + cb * 32), v1 = read_turned(src + 8 * PITCH + cb * 32);
+            const u32x4 vf = {v0.x, v0.y, v1.x, v1.y};
+#pragma unroll
+            for (int n = 0; n < T::kP; ++n) o[cb] = mma32<CT>(vf, p[n], o[cb]);
+          }
+        }
+    }
+    if (more) store(cur ^ 1);
+  }
+  l = pair_sum<32>(l);
+  if (qi >= nq) return;
+  if (hi == 0) {  // tiles that all other rows see whole were not masked for a row that sees none
+    m = -INFINITY;
+    l = 0.f;
+  }
+  m = m == -INFINITY ? m : m * f;
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int c0 = 32 * cb + 8 * r4 + 4 * half;
+      float x[4] = {o[cb][4 * r4], o[cb][4 * r4 + 1], o[cb][4 * r4 + 2], o[cb][4 * r4 + 3]};
+      const bool odd = !(fabsf(x[0]) < INFINITY && fabsf(x[1]) < INFINITY && fabsf(x[2]) < INFINITY && fabsf(x[3]) < INFINITY);
+      if (odd && l < INFINITY)
+        sum_values<CT, DH>(a, s, kvh, row, head, max(lo, begin), min(hi, end), m, a.scale * 1.44269504f, c0, x);
+      put_out(a, gr.S, split, row, head, DH, c0, m, l, x);
+    }
+}
+
+// Joins the splits' sums: one wave per (row, head); lane i looks after split i's state and
+// after DH / 64 channels (a half wave per row for 32).
+template <int DH>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttend a, int S) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t i = (int64_t)blockIdx.x * 4 + wave;
+  const int h = (int)(i % a.H), tok = (int)(i / a.H % a.r.max_rows);
+  const int64_t s = i / a.H / a.r.max_rows;
+  if (s >= a.c.n_seqs) return;
+  const SeqRows sr = seq_rows(a.r, (int)s);
+  if (tok >= sr.n) return;
+  const int64_t rows = (int64_t)a.r.n_rows * a.H, at = (int64_t)(sr.row0 + tok) * a.H + h;
+  const float2* ml = reinterpret_cast<const float2*>(a.work + rows * S * DH);
+  const float2 st = lane < S ? ml[lane * rows + at] : make_float2(-INFINITY, 0.f);
+  const float m = wave_max(st.x);
+  const bool used = !(st.x == -INFINITY && st.y == 0.f);
+  const float w = used ? __builtin_amdgcn_exp2f(st.x - m) : 0.f;
+  const float l = wave_sum(used ? w * st.y : 0.f);
+  constexpr int N = DH == 128 ? 2 : 1;
+  float o[2] = {0.f, 0.f};
+  const int c0 = (lane * N) & (DH - 1);
+  uint64_t todo = __ballot(used);
+  while (todo != 0) {
+    const int k = __builtin_ctzll(todo);
+    todo &= todo - 1;
+    const float wk = __shfl(w, k);
+    const float* p = a.work + ((int64_t)k * rows + at) * DH + c0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) o[j] += wk * p[j];
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  if (lane * N >= DH) return;
+  const int64_t dst = (int64_t)(sr.row0 + tok) * a.o.row + (int64_t)h * a.o.head + c0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const float x = l == 0.f ? 0.f : o[j] * inv;
+    if (a.o.type == PT_F32) reinterpret_cast<float*>(a.o.p)[dst + j] = x;
+    else reinterpret_cast<uint16_t*>(a.o.p)[dst + j] = (uint16_t)(a.o.type == PT_BF16 ? pack_bf16(x, 0.f) : pack_f16(x, 0.f));
+  }
+}
+
+// Few packed rows (rows of a sequence times query heads of a KV head) run on the step
+// kernel.
+constexpr int kStepRows = 32;
+constexpr int kMaxSplits = 64;
+
+struct Plan {
+  bool step;
+  Grid g;
+};
+
+Plan plan_of(const PagedCache& c, const PagedRows& r, int H) {
+  Plan p;
+  const int64_t packed = (int64_t)r.max_rows * (H / c.hk);
+  p.step = packed <= kStepRows;
+  const int64_t per = p.step ? 16 : 128;
+  p.g.tiles = (int)((packed + per - 1) / per);
+  // enough blocks for the chip's 256 compute units, of at least 256 slots each
+  const int64_t blocks = (int64_t)p.g.tiles * c.n_seqs * c.hk, slots = std::max(r.max_slots, 1);
+  const int64_t want = (p.step ? 1024 : 512) / std::max<int64_t>(blocks, 1);
+  int64_t S = std::min<int64_t>(std::min<int64_t>(want, kMaxSplits), (slots + 255) / 256);
+  S = std::max<int64_t>(S, 1);
+  p.g.chunk = (int)(((slots + S - 1) / S + 63) / 64 * 64);
+  p.g.S = (int)((slots + p.g.chunk - 1) / p.g.chunk);
+  return p;
+}
+
+template <int CT, int DH, int QT>
+hipError_t attend_at(const PagedAttend& a, const Plan& p, hipStream_t st, const Ev& ev) {
+  const dim3 grid((uint32_t)((int64_t)p.g.S * p.g.tiles * a.c.hk * a.c.n_seqs));
+  const bool join = p.g.S > 1;
+  hipError_t e;
+  if (p.step) e = plaunch(paged_step_kernel<CT, DH, QT>, grid, dim3(256), st, ev.start, join ? nullptr : ev.stop, a, p.g);
+  else e = plaunch(paged_prompt_kernel<CT, DH, QT>, grid, dim3(256), st, ev.start, join ? nullptr : ev.stop, a, p.g);
+  if (e != hipSuccess || !join) return e;
+  const int64_t waves = (int64_t)a.c.n_seqs * a.r.max_rows * a.H;
+  return plaunch(paged_join_kernel<DH>, dim3((uint32_t)((waves + 3) / 4)), dim3(256), st, nullptr, ev.stop, a, p.g.S);
+}
+
+template <int CT, int DH>
+hipError_t attend_dh(const PagedAttend& a, const Plan& p, hipStream_t st, const Ev& ev) {
+  if (a.q.type == PT_F32) return attend_at<CT, DH, PT_F32>(a, p, st, ev);
+  if constexpr (CT != PT_F16) {
+    if (a.q.type == PT_BF16) return attend_at<CT, DH, PT_BF16>(a, p, st, ev);
+  }
+  if constexpr (CT != PT_BF16) {
+    if (a.q.type == PT_F16) return attend_at<CT, DH, PT_F16>(a, p, st, ev);
+  }
+  return hipErrorInvalidValue;
+}
+
+template <int CT>
+hipError_t attend_ct(const PagedAttend& a, const Plan& p, hipStream_t st, const Ev& ev) {
+  switch (a.c.dh) {
+    case 32: return attend_dh<CT, 32>(a, p, st, ev);
+    case 64: return attend_dh<CT, 64>(a, p, st, ev);
+    case 128: return attend_dh<CT, 128>(a, p, st, ev);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace
+
+size_t paged_work_bytes(const PagedCache& c, const PagedRows& r, int H) {
+  const Plan p = plan_of(c, r, H);
+  return p.g.S > 1 ? (size_t)p.g.S * r.n_rows * H * (c.dh + 2) * 4 : 0;
+}
+
+hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st, const Ev& ev) {
+  const int units = ((a.q.p != nullptr ? a.H : 0) + 2 * a.c.hk) * (a.c.dh / 8);
+  const int64_t all = (int64_t)units * a.r.n_rows;
+  const dim3 grid((uint32_t)((all + 255) / 256));
+  switch (a.c.type) {
+    case PT_BF16: return plaunch(paged_append_kernel<PT_BF16>, grid, dim3(256), st, ev.start, ev.stop, a, units, all);
+    case PT_F16: return plaunch(paged_append_kernel<PT_F16>, grid, dim3(256), st, ev.start, ev.stop, a, units, all);
+    case PT_MXFP4: return plaunch(paged_append_kernel<PT_MXFP4>, grid, dim3(256), st, ev.start, ev.stop, a, units, all);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+hipError_t launch_paged_read(const PagedCache& c, const PagedRows& r, const HeadRows& k, const HeadRows& v, hipStream_t st,
+                             const Ev& ev) {
+  const int units = 2 * c.hk * (c.dh / 8);
+  const int64_t all = (int64_t)units * r.n_rows;
+  return plaunch(paged_read_kernel, dim3((uint32_t)((all + 255) / 256)), dim3(256), st, ev.start, ev.stop, c, r, k, v, units, all);
+}
+
+hipError_t launch_paged_attend(const PagedAttend& a, hipStream_t st, const Ev& ev) {
+  const Plan p = plan_of(a.c, a.r, a.H);
+  switch (a.c.type) {
+    case PT_BF16: return attend_ct<PT_BF16>(a, p, st, ev);
+    case PT_F16: return attend_ct<PT_F16>(a, p, st, ev);
+    case PT_MXFP4: return attend_ct<PT_MXFP4>(a, p, st, ev);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace mbp
