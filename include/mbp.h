@@ -90,9 +90,14 @@ typedef enum { MBP_ACCEPT_THRESHOLD = 0, MBP_ACCEPT_SELF_VERIFY = 1 } mbp_mode;
  *                             their caches for every position (max_window defaults to
  *                             max_ctx + max_n; its first update runs the whole prefix).
  *                             Other values: MBP_EINVAL.
- *   kv_dtype                  storage type of every KV cache: MBP_F32, MBP_BF16 or
- *                             MBP_F16.  MBP_F16 stores the same bytes as bf16 with 3
- *                             more mantissa bits; values beyond +-65504 saturate.
+ *   kv_dtype                  storage type of every KV cache: MBP_F32, MBP_BF16,
+ *                             MBP_F16 or MBP_MXFP4.  MBP_F16 stores the same bytes as
+ *                             bf16 with 3 more mantissa bits; values beyond +-65504
+ *                             saturate.  MBP_MXFP4 keeps the encoder's, LM module's and
+ *                             next-byte decoder's keys and values in 4.25 bits, in
+ *                             pages of 64 slots (the format of mbp_paged_cache), and
+ *                             the MB window's, a few dozen rows, in float16; every
+ *                             pass then runs one kernel per layer operation.
  *   no_engine                 0: passes of at most 16 token rows through a
  *                             transformer stack run in the persistent engine (one
  *                             launch per stack, layers chained through

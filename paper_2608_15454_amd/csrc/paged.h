@@ -64,6 +64,7 @@ struct PagedAttend {
 };
 
 size_t paged_work_bytes(const PagedCache& c, const PagedRows& r, int H);
+size_t paged_work_most(int dh);  // no call with a full row of heads in every tile needs more
 hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st, const Ev& ev = Ev());
 // The inverse: all n_rows rows of k and v receive the values of their slots (0 for a row
 // of no sequence or a slot without a page).

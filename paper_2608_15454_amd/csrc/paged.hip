@@ -1036,6 +1036,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttend a, int S) {
 // kernel.
 constexpr int kStepRows = 32;
 constexpr int kMaxSplits = 64;
+// blocks of a launch up to which the slots are split
+constexpr int kStepBlocks = 1024, kPromptBlocks = 512;
 
 struct Plan {
   bool step;
@@ -1050,7 +1052,7 @@ Plan plan_of(const PagedCache& c, const PagedRows& r, int H) {
   p.g.tiles = (int)((packed + per - 1) / per);
   // enough blocks for the chip's 256 compute units, of at least 256 slots each
   const int64_t blocks = (int64_t)p.g.tiles * c.n_seqs * c.hk, slots = std::max(r.max_slots, 1);
-  const int64_t want = (p.step ? 1024 : 512) / std::max<int64_t>(blocks, 1);
+  const int64_t want = (p.step ? kStepBlocks : kPromptBlocks) / std::max<int64_t>(blocks, 1);
   int64_t S = std::min<int64_t>(std::min<int64_t>(want, kMaxSplits), (slots + 255) / 256);
   S = std::max<int64_t>(S, 1);
   p.g.chunk = (int)(((slots + S - 1) / S + 63) / 64 * 64);
@@ -1097,6 +1099,11 @@ hipError_t attend_ct(const PagedAttend& a, const Plan& p, hipStream_t st, const 
 size_t paged_work_bytes(const PagedCache& c, const PagedRows& r, int H) {
   const Plan p = plan_of(c, r, H);
   return p.g.S > 1 ? (size_t)p.g.S * r.n_rows * H * (c.dh + 2) * 4 : 0;
+}
+
+// A split launch has at most so many blocks, of 16 or 128 packed rows each.
+size_t paged_work_most(int dh) {
+  return (size_t)std::max(16 * kStepBlocks, 128 * kPromptBlocks) * (dh + 2) * 4;
 }
 
 hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st, const Ev& ev) {

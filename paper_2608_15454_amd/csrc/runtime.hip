@@ -27,6 +27,7 @@
 #include "engine.h"
 #include "kernels.h"
 #include "mbp.h"
+#include "paged.h"
 
 using namespace mbp;
 
@@ -80,7 +81,14 @@ struct KV {  // one module's KV cache: layer l of row b at k + l*layer_stride + 
   void* v = nullptr;
   int64_t layer_stride = 0, b_stride = 0;
   int32_t cap = 0;
+  // 4-bit caches: a page table of its own rows' pages in order, shared by the layers,
+  // whose pools are layer_stride bytes apart
+  const int32_t* pages = nullptr;
+  int32_t max_pages = 0;
 };
+
+// Slots of a page of a handle's own 4-bit caches.
+constexpr int kPageShift = 6;
 
 // last_mode of a pending step made by mbp_verify_draft
 constexpr int kModeExternal = 2;
@@ -110,7 +118,9 @@ struct Row {
 struct Sizes {
   int d, H, dh, dff, B, Tcap, Kcap, Wcap, Mc, Ml, Mm, nmax, Smax;
   int64_t part_floats, part_floats_mb;
-  size_t es;  // element size of the KV caches
+  size_t es;   // element size of the KV caches (4-bit caches: of the MB window's)
+  bool fp4;    // the encoder's, LM module's and NT decoder's caches are MXFP4 pages
+  int Tpages, Kpages;  // pages of a row's bytes and latents there
   int Esplit;          // attention splits per (row, head) the engine buffers hold
   int64_t ll_set;      // tagged 8-byte entries of one set of engine buffers
   int64_t ll_entries;  // all sets
@@ -134,7 +144,7 @@ constexpr int kPlans = 3;  // 0 commit, 1 window update and head of a step, 2 fo
 
 struct Regions {
   size_t gains, rope, enc_k, enc_v, lm_k, lm_v, nt_k, nt_v, mb_k, mb_v, he, lat_in, lat_out, rows, logits, vlogits,
-      Xl, active, total;
+      Xl, active, stage, iota, pages_t, pages_k, total;
   ScratchOff main, mb;
   size_t plan[kPlans];
   size_t plan_ints;
@@ -169,9 +179,11 @@ bool valid_cfg(const mbp_config* c, std::string* why) {
     return bad("max_window must be given when max_patch = 0");
   if (c->max_chunk < 0) return bad("max_chunk must be >= 0");
   if (c->window_mode != 0 && c->window_mode != 1) return bad("window_mode must be 0 or 1");
-  if (c->kv_dtype != MBP_F32 && c->kv_dtype != MBP_BF16 && c->kv_dtype != MBP_F16) return bad("bad kv_dtype");
+  if (c->kv_dtype != MBP_F32 && c->kv_dtype != MBP_BF16 && c->kv_dtype != MBP_F16 && c->kv_dtype != MBP_MXFP4) return bad("bad kv_dtype");
   if (c->no_engine != 0 && c->no_engine != 1) return bad("no_engine must be 0 or 1");
   if (c->boundary_mode != 0 && c->boundary_mode != 1) return bad("boundary_mode must be 0 or 1");
+  if (c->kv_dtype == MBP_MXFP4 && (c->max_ctx > (1 << 30) - 64 || (int64_t)c->max_batch * (c->max_ctx / 64 + 2) > INT32_MAX))
+    return bad("max_batch x max_ctx too large for 4-bit caches");
   if (!(c->rope_base > 0.f) || !(c->rms_eps >= 0.f) || !std::isfinite(c->attn_scale)) return bad("bad rope_base/rms_eps/attn_scale");
   return true;
 }
@@ -202,6 +214,10 @@ Sizes sizes_of(const mbp_config& c) {
   const int sw = (s.Wcap + 255) / 256;
   s.part_floats_mb = sw > 1 ? (int64_t)s.Mm * s.H * sw * (s.dh + 2) : 0;
   s.es = c.kv_dtype == MBP_F32 ? 4 : 2;
+  s.fp4 = c.kv_dtype == MBP_MXFP4;
+  s.Tpages = (s.Tcap + (1 << kPageShift) - 1) >> kPageShift;
+  s.Kpages = (s.Kcap + (1 << kPageShift) - 1) >> kPageShift;
+  if (s.fp4) s.part_floats = std::max<int64_t>(s.part_floats, (int64_t)(paged_work_most(s.dh) / 4));
   const int ex = kEngineMaxRows;
   s.Esplit = kEngineMaxSplits;
   s.ll_set = (int64_t)ex * s.d * 7 + (int64_t)ex * s.dff + (int64_t)ex * s.H * s.Esplit * (s.dh + 2);
@@ -210,6 +226,9 @@ Sizes sizes_of(const mbp_config& c) {
   s.eng_ops = 6 * (c.n_enc + c.n_lm + c.n_nb + (c.head == MBP_HEAD_LCA ? c.n_mb : 0));
   return s;
 }
+
+// Bytes of one head's page of a 4-bit cache.
+size_t page_bytes4(const Sizes& s) { return (size_t)(s.dh / 2 + s.dh / 32) << kPageShift; }
 
 int n_gain_vectors(const mbp_config& c) {
   int n = 2 * (c.n_enc + c.n_lm + c.n_nb) + 1 /*nt_norm*/ + 1 /*bos*/;
@@ -231,8 +250,8 @@ Regions layout(const mbp_config& c) {
   const int npos = std::max(s.Tcap + s.nmax, s.Kcap) + 1;
   r.gains = take((size_t)n_gain_vectors(c) * s.d * 4);
   r.rope = take((size_t)npos * (s.dh / 2) * 8);
-  const size_t kv_bt = (size_t)s.B * s.Tcap * s.d * s.es;
-  const size_t kv_bk = (size_t)s.B * s.Kcap * s.d * s.es;
+  const size_t kv_bt = s.fp4 ? (size_t)s.B * s.Tpages * page_bytes4(s) * s.H : (size_t)s.B * s.Tcap * s.d * s.es;
+  const size_t kv_bk = s.fp4 ? (size_t)s.B * s.Kpages * page_bytes4(s) * s.H : (size_t)s.B * s.Kcap * s.d * s.es;
   const size_t kv_bw = (size_t)s.B * s.Wcap * s.d * s.es;
   r.enc_k = take(kv_bt * c.n_enc);
   r.enc_v = take(kv_bt * c.n_enc);
@@ -273,6 +292,14 @@ Regions layout(const mbp_config& c) {
   r.mb.part = take((size_t)std::max<int64_t>(s.part_floats_mb, 1) * 4);
   r.mb.gpart = take((size_t)kGemmPartFloats * 4);
   r.plan_ints = (size_t)40 * s.Ml + (size_t)2 * s.B * s.Wcap + 256;
+  if (s.fp4) {
+    r.plan_ints += (size_t)4 * s.B + 64;  // row starts and first slots of two passes
+    // a pass's rotated keys and its values before they are stored, [H][rows][dh] each
+    r.stage = take((size_t)2 * s.Ml * s.d * 4);
+    r.iota = take((size_t)s.Ml * 4);
+    r.pages_t = take((size_t)s.B * s.Tpages * 4);
+    r.pages_k = take((size_t)s.B * s.Kpages * 4);
+  }
   for (int i = 0; i < kPlans; ++i) r.plan[i] = take(r.plan_ints * 4);
   r.active = take((size_t)s.B * 4);
   r.ll = take((size_t)s.ll_entries * 8);
@@ -380,6 +407,9 @@ struct TokOffs {
   size_t first;       // index of the first token of the same batch row (rows are contiguous)
   size_t first_slot;  // slot of that token
   int32_t max_ns;     // largest such slot
+  // 4-bit caches: the pass's rows by batch row (PagedRows)
+  size_t row_start, first_of_row;
+  int32_t max_rows;
 };
 
 }  // namespace
@@ -422,6 +452,8 @@ struct mbp_handle {
   KV kv_enc, kv_lm, kv_nt, kv_mb;
   float2* rope;
   Scratch sc_main, sc_mb;
+  float* stage = nullptr;  // 4-bit caches: keys and values of a pass before they are stored
+  const int32_t* iota = nullptr;
 
   std::vector<Row> rows;
   int batch = 0;
@@ -548,7 +580,7 @@ double linear_bytes(const mbp_handle* h, const Linear& L) {
     case EPI_STORE: out = M * N * 4; break;
     case EPI_RESID: out = 2 * M * N * 4; break;
     case EPI_SWIGLU: out = M * (N / 2) * 4; break;
-    default: out = M * (N / 3) * 4 + 2 * M * (N / 3) * (double)h->sz.es; break;
+    default: out = M * (N / 3) * 4 + 2 * M * (N / 3) * (L.epi.kvt == PT_F32 ? 4.0 : 2.0); break;
   }
   return N * K * wb + M * K * 4 + out;
 }
@@ -590,8 +622,9 @@ int upload(mbp_handle* h, Plan& p, hipStream_t st, size_t from = 0) {
   return MBP_OK;
 }
 
-TokOffs add_toks(Plan& p, const Toks& t) {
-  TokOffs o;
+// batch: rows of the batch where the pass's stack has 4-bit caches, else 0.
+TokOffs add_toks(Plan& p, const Toks& t, int batch = 0) {
+  TokOffs o{};
   o.b = p.add(t.b);
   o.pos = p.add(t.pos);
   o.slot = p.add(t.slot);
@@ -618,7 +651,24 @@ TokOffs add_toks(Plan& p, const Toks& t) {
   }
   o.qg = p.add(qg);
   o.nqg = (int32_t)qg.size() / 2;
+  if (batch > 0) {  // tokens come in batch-row order, each row's in consecutive slots
+    std::vector<int32_t> start(batch + 1), slot(batch, 0);
+    int i = 0;
+    for (int b = 0; b < batch; ++b) {
+      start[b] = i;
+      if (i < t.size() && t.b[i] == b) slot[b] = t.slot[i];
+      while (i < t.size() && t.b[i] == b) ++i;
+      o.max_rows = std::max(o.max_rows, i - start[b]);
+    }
+    start[batch] = i;
+    o.row_start = p.add(start);
+    o.first_of_row = p.add(slot);
+  }
   return o;
+}
+
+PagedRows dev_rows(const Plan& p, const TokOffs& o, int M, int max_kv) {
+  return PagedRows{p.at(o.row_start), p.at(o.first_of_row), M, o.max_rows, max_kv};
 }
 
 Tok dev_tok(const Plan& p, const TokOffs& o, int M) {
@@ -658,7 +708,7 @@ double stack_bytes(const mbp_handle* h, int nlayers, int M, double kv_rows) {
   const double per_layer = (4.0 * d * d + 3.0 * d * f) * wb        // weights
                            + M * (d * 4 + d * 4 + d * 4 + f * 4) * 4.0  // linear inputs
                            + M * (3 * d + 2 * d + f + 2 * d) * 4.0       // outputs and residual reads
-                           + kv_rows * 2.0 * d * (double)s.es;           // attention K/V
+                           + kv_rows * 2.0 * d * (s.fp4 ? 17.0 / 32 : (double)s.es);  // attention K/V
   return per_layer * nlayers;
 }
 
@@ -742,18 +792,20 @@ int run_engine_split(mbp_handle* h, const EngStack& ea, int la, const ECall& ca,
 // its queries see them.
 int run_stack(mbp_handle* h, const std::vector<BlockW>& layers, const KV& kv, float* X, const Tok& tok,
               const int32_t* grp_tab, bool tiled, const int32_t* tiles, int ntiles, int max_kv, double kv_rows,
-              const Scratch& sc, hipStream_t st) {
+              const Scratch& sc, hipStream_t st, const PagedRows& pr) {
   const Sizes& s = h->sz;
   const int M = tok.M;
   if (M == 0) return MBP_OK;
+  const bool paged = kv.pages != nullptr;
+  const int kvt = s.fp4 ? (int)PT_F16 : h->cfg.kv_dtype;  // 4-bit caches: the MB window's
   const float scale = h->cfg.attn_scale / std::sqrt((float)s.dh);
   uint16_t* const so = reinterpret_cast<uint16_t*>(sc.O);
   uint16_t* const sh = reinterpret_cast<uint16_t*>(sc.Hid);
   bool normed = false;  // sc.O holds the split rows of the layer's normed input
   for (size_t l = 0; l < layers.size(); ++l) {
     const BlockW& w = layers[l];
-    char* kc = reinterpret_cast<char*>(kv.k) + l * kv.layer_stride * s.es;
-    char* vc = reinterpret_cast<char*>(kv.v) + l * kv.layer_stride * s.es;
+    char* kc = reinterpret_cast<char*>(kv.k) + l * kv.layer_stride * (paged ? 1 : s.es);
+    char* vc = reinterpret_cast<char*>(kv.v) + l * kv.layer_stride * (paged ? 1 : s.es);
     Linear qkv{};
     qkv.X = X; qkv.ldx = s.d; qkv.M = M; qkv.K = s.d; qkv.N = 3 * s.d;
     qkv.gain = w.attn_norm; qkv.eps = h->cfg.rms_eps;
@@ -761,7 +813,15 @@ int run_stack(mbp_handle* h, const std::vector<BlockW>& layers, const KV& kv, fl
     qkv.mats.rows = s.d; qkv.mats.mode = MAT_QKV;
     qkv.epi.kind = EPI_QKV; qkv.epi.Q = sc.Q; qkv.epi.kc = kc; qkv.epi.vc = vc;
     qkv.epi.b_stride = kv.b_stride; qkv.epi.cap = kv.cap; qkv.epi.H = s.H; qkv.epi.dh = s.dh; qkv.epi.d = s.d;
-    qkv.epi.rope = h->rope; qkv.epi.tok = tok; qkv.epi.kvt = h->cfg.kv_dtype;
+    qkv.epi.rope = h->rope; qkv.epi.tok = tok; qkv.epi.kvt = kvt;
+    if (paged) {  // the rotated keys and the values in float32, row i at slot i of one cache
+      qkv.epi.kc = h->stage;
+      qkv.epi.vc = h->stage + (size_t)M * s.d;
+      qkv.epi.b_stride = 0;
+      qkv.epi.cap = M;
+      qkv.epi.tok.slot = h->iota;
+      qkv.epi.kvt = PT_F32;
+    }
     Linear o{};
     o.X = sc.O; o.ldx = s.d; o.M = M; o.K = s.d; o.N = s.d; o.gain = nullptr;
     o.mats.m[0] = w.wo; o.mats.rows = s.d; o.mats.mode = MAT_SINGLE;
@@ -790,11 +850,28 @@ int run_stack(mbp_handle* h, const std::vector<BlockW>& layers, const KV& kv, fl
     Attn a{};
     a.Q = sc.Q; a.ldq = s.d; a.kc = kc; a.vc = vc; a.b_stride = kv.b_stride; a.cap = kv.cap;
     a.H = s.H; a.dh = s.dh; a.tok = tok; a.grp_tab = grp_tab; a.scale = scale; a.O = sc.O; a.ldo = s.d; a.split = planes ? 1 : 0;
-    const double abytes = kv_rows * 2.0 * s.d * (double)s.es + 2.0 * M * s.d * 4;
-    if (tiled) {
-      TIMED(h, MBP_KCLASS_ATTN, abytes, launch_attn_prefill, a, h->cfg.kv_dtype, tiles, ntiles, max_kv, st);
+    const double abytes = kv_rows * 2.0 * s.d * (paged ? 17.0 / 32 : (double)s.es) + 2.0 * M * s.d * 4;
+    if (paged) {
+      const PagedCache pc{kc, vc, kv.pages, PT_MXFP4, s.H, s.dh, kPageShift, h->cfg.max_batch * kv.max_pages, h->batch,
+                          kv.max_pages, (int64_t)page_bytes4(s)};
+      PagedAppend ap{};
+      ap.c = pc; ap.r = pr;
+      ap.k = HeadRows{h->stage, s.dh, (int64_t)M * s.dh, PT_F32, 1};
+      ap.v = HeadRows{h->stage + (size_t)M * s.d, s.dh, (int64_t)M * s.dh, PT_F32, 1};
+      OTHER(h, launch_paged_append, ap, st);
+      PagedAttend pa{};
+      pa.c = pc; pa.r = pr; pa.H = s.H; pa.scale = scale; pa.work = sc.part;
+      pa.q = HeadRows{sc.Q, s.d, s.dh, PT_F32, 1};
+      // the appended rows' staging is free again: outputs that the next product wants as
+      // split rows go there first
+      pa.o = HeadRows{planes ? h->stage : sc.O, s.d, s.dh, PT_F32, 1};
+      if (paged_work_bytes(pc, pr, s.H) > (size_t)sc.part_floats * 4) return fail(h, MBP_ECAPACITY, "attention scratch exceeds its region");
+      TIMED(h, MBP_KCLASS_ATTN, abytes, launch_paged_attend, pa, st);
+      if (planes) OTHER(h, launch_split_rows, h->stage, nullptr, 0.f, so, nullptr, s.d, M, st);
+    } else if (tiled) {
+      TIMED(h, MBP_KCLASS_ATTN, abytes, launch_attn_prefill, a, kvt, tiles, ntiles, max_kv, st);
     } else {
-      TIMED(h, MBP_KCLASS_ATTN, abytes, launch_attn_decode, a, h->cfg.kv_dtype, max_kv, sc.part, sc.part_floats, st);
+      TIMED(h, MBP_KCLASS_ATTN, abytes, launch_attn_decode, a, kvt, max_kv, sc.part, sc.part_floats, st);
     }
 
     if (planes) {
@@ -821,7 +898,7 @@ int run_stack(mbp_handle* h, const std::vector<BlockW>& layers, const KV& kv, fl
 int run_pass(mbp_handle* h, const std::vector<BlockW>& layers, const KV& kv, const EngStack* es, const EIo& io,
              float* X, const Tok& tok, const int32_t* grp_tab, bool tiled, const int32_t* tiles, int ntiles,
              int max_kv, double kv_rows, const Scratch& sc, hipStream_t st, const int32_t* first,
-             const int32_t* first_slot, int32_t max_ns) {
+             const int32_t* first_slot, int32_t max_ns, const PagedRows& pr = PagedRows()) {
   const Sizes& s = h->sz;
   const int M = tok.M;
   if (M == 0) return MBP_OK;
@@ -833,7 +910,7 @@ int run_pass(mbp_handle* h, const std::vector<BlockW>& layers, const KV& kv, con
   } else if (io.xa != X || io.ia != nullptr || io.xb != nullptr) {
     OTHER(h, launch_copy_rows, io.xa, io.ia, io.xb, io.ib, X, nullptr, s.d, M, st);
   }
-  RCK(run_stack(h, layers, kv, X, tok, grp_tab, tiled, tiles, ntiles, max_kv, kv_rows, sc, st));
+  RCK(run_stack(h, layers, kv, X, tok, grp_tab, tiled, tiles, ntiles, max_kv, kv_rows, sc, st, pr));
   if (io.xo != X || io.oi != nullptr) OTHER(h, launch_copy_rows, X, nullptr, nullptr, nullptr, io.xo, io.oi, s.d, M, st);
   if (io.oi2 != nullptr) OTHER(h, launch_copy_rows, X, nullptr, nullptr, nullptr, io.xo2, io.oi2, s.d, M, st);
   return MBP_OK;
@@ -1072,7 +1149,8 @@ int commit(mbp_handle* h, const std::vector<std::vector<uint8_t>>& add, bool for
     std::vector<int32_t> tiles_e = make_tiles(te);
     Plan& p = h->plan[0];
     p.clear();
-    const TokOffs oe = add_toks(p, te);
+    const int paged_rows = s.fp4 ? h->batch : 0;
+    const TokOffs oe = add_toks(p, te, paged_rows);
     const size_t o_bytes = p.add(bytes), o_he = p.add(he_row), o_h1 = p.add(h1_dst), o_te = p.add(tiles_e);
     auto encoder = [&]() -> int {  // embeddings of the new bytes -> h_e rows
       const Tok tok_e = dev_tok(p, oe, Me);
@@ -1084,7 +1162,7 @@ int commit(mbp_handle* h, const std::vector<std::vector<uint8_t>>& add, bool for
       ioe.oi = p.at(o_he);
       return run_pass(h, h->enc, h->kv_enc, &h->es_enc, ioe, X, tok_e, nullptr, tiled_e, p.at(o_te),
                       (int)tiles_e.size() / 2, max_kv_e, kvr_e, sc, h->st, p.at(oe.first), p.at(oe.first_slot),
-                      oe.max_ns);
+                      oe.max_ns, dev_rows(p, oe, Me, max_kv_e));
     };
     size_t tail = 0;
     if (learned) {
@@ -1138,7 +1216,7 @@ int commit(mbp_handle* h, const std::vector<std::vector<uint8_t>>& add, bool for
     const int Ml = tl.size();
     const bool tiled_l = Ml >= 16 * (int)rows_in_chunk.size();
     std::vector<int32_t> tiles_l = make_tiles(tl);
-    const TokOffs ol = add_toks(p, tl);
+    const TokOffs ol = add_toks(p, tl, paged_rows);
     const size_t o_nts = p.add(nt_src), o_lo = p.add(lo_row), o_cnt = p.add(cnt), o_lat = p.add(lat_row),
                  o_tl = p.add(tiles_l);
     const bool pre_here = pre && last == items.size();
@@ -1164,7 +1242,7 @@ int commit(mbp_handle* h, const std::vector<std::vector<uint8_t>>& add, bool for
       iol.oi = p.at(o_lat);
       RCK(run_pass(h, h->lm, h->kv_lm, &h->es_lm, iol, Xl, tok_l, nullptr, tiled_l, p.at(o_tl),
                    (int)tiles_l.size() / 2, max_kv_l, kvr_l, sc, h->st, p.at(ol.first), p.at(ol.first_slot),
-                   ol.max_ns));
+                   ol.max_ns, dev_rows(p, ol, Ml, max_kv_l)));
     }
     const bool fork_here = fork && last == items.size();
     if (fork_here) HIPCK(h, hipEventRecord(h->ev_fork, h->st));  // the latents are final here
@@ -1196,7 +1274,7 @@ int commit(mbp_handle* h, const std::vector<std::vector<uint8_t>>& add, bool for
     if (!split)
       RCK(run_pass(h, h->nt, h->kv_nt, &h->es_nt, ion, X, tok_e, nullptr, tiled_e, p.at(o_te),
                    (int)tiles_e.size() / 2, max_kv_e, kvr_e, sc, h->st, p.at(oe.first), p.at(oe.first_slot),
-                   oe.max_ns));
+                   oe.max_ns, dev_rows(p, oe, Me, max_kv_e)));
     if (pre_here) {
       if (!split) RCK(mb_launch(h, p, mp_next, h->st));
       h->pre_draft = true;
@@ -1367,7 +1445,7 @@ int draft(mbp_handle* h, int n, float tau, bool threshold, uint8_t* d_cand, floa
 int build_engine(mbp_handle* h) {
   const Sizes& s = h->sz;
   const mbp_config& c = h->cfg;
-  if (c.no_engine) return MBP_OK;
+  if (c.no_engine || s.fp4) return MBP_OK;  // the engine reads no 4-bit pages
   const int shape = engine_shape(h->wdt, c.kv_dtype, s.dh, s.d, s.dff);
   if (shape < 0 || engine_grid(shape) <= 0) return MBP_OK;
   h->eng_shape = shape;
@@ -1611,6 +1689,29 @@ extern "C" int mbp_init(const mbp_config* cfg, const void* const* d_weights, int
   h->kv_nt = kvof(rg.nt_k, rg.nt_v, s.Tcap);
   h->kv_lm = kvof(rg.lm_k, rg.lm_v, s.Kcap);
   h->kv_mb = kvof(rg.mb_k, rg.mb_v, s.Wcap);
+  if (s.fp4) {
+    // every row's pages in order
+    std::vector<int32_t> up(std::max({(size_t)s.B * s.Tpages, (size_t)s.B * s.Kpages, (size_t)s.Ml}));
+    for (size_t i = 0; i < up.size(); ++i) up[i] = (int32_t)i;
+    auto put = [&](size_t off, size_t n) {
+      if (e == hipSuccess) e = hipMemcpyAsync(h->ws + off, up.data(), n * 4, hipMemcpyHostToDevice, h->st);
+    };
+    put(rg.pages_t, (size_t)s.B * s.Tpages);
+    put(rg.pages_k, (size_t)s.B * s.Kpages);
+    put(rg.iota, (size_t)s.Ml);
+    if (e == hipSuccess) e = hipStreamSynchronize(h->st);
+    if (e != hipSuccess) return bail();
+    auto paged = [&](KV& k, size_t table, int pages) {
+      k.pages = h->R<int32_t>(table);
+      k.max_pages = pages;
+      k.layer_stride = (int64_t)s.B * pages * s.H * (int64_t)page_bytes4(s);
+    };
+    paged(h->kv_enc, rg.pages_t, s.Tpages);
+    paged(h->kv_nt, rg.pages_t, s.Tpages);
+    paged(h->kv_lm, rg.pages_k, s.Kpages);
+    h->stage = h->R<float>(rg.stage);
+    h->iota = h->R<int32_t>(rg.iota);
+  }
   auto scratch = [&](const ScratchOff& o, int64_t pf) {
     Scratch x;
     x.X = h->R<float>(o.X);

@@ -11,17 +11,15 @@ HALF_STEP = {"f32": 2.0**-24, "bf16": 2.0**-8, "f16": 2.0**-11}
 def to_mxfp4(x):
     """x [..., d] -> the values its codes stand for (blocks of 32 channels)."""
     b = np.asarray(x, np.float64).reshape(*x.shape[:-1], -1, 32)
-    out = np.full(b.shape, np.nan)
-    amax = np.abs(b).max(-1)
-    for i in np.ndindex(amax.shape):
-        if not np.isfinite(amax[i]):
-            continue
-        e = -127 if amax[i] == 0 else int(np.clip(np.floor(np.log2(amax[i])) - 2, -127, 127))
-        for c in range(32):
-            y = abs(b[i][c]) / 2.0**e
-            near = np.abs(GRID - min(y, 6.0))
-            best = min(range(8), key=lambda k: (near[k], k % 2))  # ties to the even code
-            out[i][c] = np.copysign(GRID[best] * 2.0**e, b[i][c])
+    amax = np.abs(b).max(-1, keepdims=True)
+    fine = np.isfinite(amax)
+    safe = np.where(fine & (amax > 0), amax, 1.0)
+    e = np.where(fine & (amax > 0), np.clip(np.frexp(safe)[1] - 3, -127, 127), -127)  # floor(log2 amax) - 2
+    y = np.minimum(np.abs(np.where(fine, b, 0.0)) / 2.0**e, 6.0)
+    off = np.abs(y[..., None] - GRID)
+    even_first = [0, 2, 4, 6, 1, 3, 5, 7]  # argmin takes the first of two equally near: the even code
+    code = np.array(even_first)[np.argmin(off[..., even_first], -1)]
+    out = np.where(fine, np.copysign(GRID[code] * 2.0**e, b), np.nan)
     return out.reshape(x.shape)
 
 
