@@ -369,7 +369,8 @@ const char *mbp_last_error(const mbp_handle *h);
  *   n_kv_heads, d_head   heads and channels (32, 64 or 128).
  *   page_size   slots of a page: a power of two, 16 to 1024.
  *   n_pages     pages of each pool.
- *   n_seqs, max_pages   the page table's rows and columns; max_pages x page_size <= 2^30.
+ *   n_seqs, max_pages   the page table's rows (at most 65535) and columns; max_pages x
+ *               page_size <= 2^30.
  *   d_k, d_v    pools, each [n_pages][n_kv_heads] pages of one head, aligned to 16 bytes:
  *               [page_size][d_head] 16-bit values, or [page_size][d_head / 2] bytes of
  *               codes (channel 2j in the low half of byte j) followed by

@@ -423,16 +423,22 @@ __device__ __forceinline__ float cache_at(const char* page, int shift, int at, i
   return c & 1 ? hi_bf16(__builtin_bit_cast(uint32_t, b)) : lo_bf16(__builtin_bit_cast(uint32_t, b));
 }
 
-// Largest and smallest over 16 neighbouring lanes.
+// Largest and smallest over 16 neighbouring lanes (a row of the vector ALU).
+template <int CTRL>
+__device__ __forceinline__ int dpp_int(int x) {
+  return __builtin_amdgcn_mov_dpp(x, CTRL, 0xF, 0xF, false);
+}
 __device__ __forceinline__ int min16(int x) {
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) x = min(x, __shfl_xor(x, o));
-  return x;
+  x = min(x, dpp_int<kDppXor1>(x));
+  x = min(x, dpp_int<kDppXor2>(x));
+  x = min(x, dpp_int<kDppMirror7>(x));
+  return min(x, dpp_int<kDppMirror15>(x));
 }
 __device__ __forceinline__ int max16(int x) {
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) x = max(x, __shfl_xor(x, o));
-  return x;
+  x = max(x, dpp_int<kDppXor1>(x));
+  x = max(x, dpp_int<kDppXor2>(x));
+  x = max(x, dpp_int<kDppMirror7>(x));
+  return max(x, dpp_int<kDppMirror15>(x));
 }
 
 // The value sums of N channels from c0 on, one visible slot after the other.  A matrix
@@ -474,9 +480,15 @@ __device__ __forceinline__ void row_range(const PagedAttend& a, const SeqRows& s
   }
 }
 
-struct Grid {  // of an attention launch, one-dimensional: split fastest, then KV head, tile, sequence
-  int32_t S, chunk, tiles;
+struct Grid {  // of an attention launch: x is split fastest, then tile; y the KV head; z the sequence
+  int32_t S, chunk, tiles, G;
 };
+
+// Probabilities are 2^(f s - f m) with a reference m that need not be the largest score:
+// it follows once one is more than 2^kSlack times as probable, so that the sums are
+// rescaled a few times in a row's life instead of at every block.  2^8 keeps float16
+// terms far from the type's ends.
+constexpr float kSlack = 8.f;
 
 // Where a row's channels go: the output, or this split's sums.
 template <int N>
@@ -494,6 +506,12 @@ __device__ __forceinline__ void put_out(const PagedAttend& a, int S, int split, 
   if (c0 == 0) reinterpret_cast<float2*>(a.work + all * dh)[i] = make_float2(m, l);
 }
 
+// Waves per SIMD that a step kernel's registers leave room for without spills.
+constexpr int step_waves(int ct, int dh, int qt) {
+  if (dh < 128) return ct == PT_MXFP4 && dh == 64 && qt == PT_F32 ? 3 : 4;
+  return ct != PT_MXFP4 ? 2 : qt == PT_BF16 ? 4 : 3;
+}
+
 // Up to 16 query rows of one sequence and KV head (its rows times the query heads of the
 // group, row-major) against the slots of one split.  Four waves take blocks of KT slots in
 // turn and join their softmax states at the end.  Computed transposed, so that lane l
@@ -506,8 +524,8 @@ __device__ __forceinline__ void put_out(const PagedAttend& a, int S, int split, 
 //   O^T += V^T P^T: the probabilities are already where the product wants them, values
 //     go through the wave's own LDS tile and are read turned round.
 // The next block's loads are in flight during a block's softmax and value product.
-template <int CT, int DH, int QT>
-__global__ __launch_bounds__(256) void paged_step_kernel(PagedAttend a, Grid gr) {
+template <int CT, int DH, int QT, int NW>
+__global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_kernel(PagedAttend a, Grid gr) {
   using T = Terms<CT, QT>;
   constexpr bool F4 = CT == PT_MXFP4;
   constexpr int KT = DH == 128 ? 32 : F4 || DH == 32 ? 64 : 32;
@@ -515,57 +533,27 @@ __global__ __launch_bounds__(256) void paged_step_kernel(PagedAttend a, Grid gr)
   constexpr int VU = F4 ? KT * DH / 32 / 64 : KT * DH / 8 / 64;  // 16-byte pieces of a block's values per lane
   static_assert(VU >= 1, "a block has a piece for every lane");
   constexpr int TILE = KT * PITCH * 2, MERGE = 16 * (DH + 4) * 4;
-  __shared__ __attribute__((aligned(16))) char lds[4 * (TILE > MERGE ? TILE : MERGE)];
+  __shared__ __attribute__((aligned(16))) char lds[NW * (TILE > MERGE ? TILE : MERGE)];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
-  int bid = blockIdx.x;
-  const int split = bid % gr.S;
-  bid /= gr.S;
-  const int kvh = bid % a.c.hk;
-  bid /= a.c.hk;
-  const int tile = bid % gr.tiles, s = bid / gr.tiles;
-  const int G = a.H / a.c.hk;
+  const int tile = gr.tiles == 1 ? 0 : blockIdx.x / gr.S, split = blockIdx.x - tile * gr.S, kvh = blockIdx.y, s = blockIdx.z;
+  const int G = gr.G;
   const SeqRows sr = seq_rows(a.r, s);
   const int nq = min(sr.n, a.r.max_rows) * G;
   if (tile * 16 >= nq) return;
   const int cap = a.c.max_pages << a.c.shift;
-  const int qi = tile * 16 + col, tok = min(qi, nq - 1) / G, head = kvh * G + min(qi, nq - 1) - tok * G, row = sr.row0 + tok;
+  const int qi = tile * 16 + col, tok = G == 1 ? min(qi, nq - 1) : min(qi, nq - 1) / G,
+            head = kvh * G + min(qi, nq - 1) - tok * G, row = sr.row0 + tok;
+  float x[KS][8];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+    load8(a.q.p, (int64_t)row * a.q.row + (int64_t)head * a.q.head + g * (DH / 4) + ks * 8, QT, a.q.vec, x[ks]);
   int lo = cap, hi = 0;
   if (qi < nq) row_range(a, sr, tok, cap, &lo, &hi);
   const int kmin = __builtin_amdgcn_readfirstlane(min16(lo)), kmax = __builtin_amdgcn_readfirstlane(max16(hi));
   const int lo_all = __builtin_amdgcn_readfirstlane(max16(hi > 0 ? lo : 0)), hi_all = __builtin_amdgcn_readfirstlane(min16(hi > 0 ? hi : cap));
   const int64_t b0 = (int64_t)(kmin & ~(KT - 1)) + (int64_t)split * gr.chunk;
-  const int begin = (int)min(b0, (int64_t)cap);
-  const int end = split == gr.S - 1 ? kmax : (int)min((int64_t)kmax, b0 + gr.chunk);
-
-  // queries: channels g DH / 4 + 8 ks .. +7 of row col in step ks
-  float f = a.scale * 1.44269504f;  // probabilities are 2^(f s - f max)
-  float sign = f < 0.f ? -1.f : f == 0.f ? 0.f : 1.f;
-  f = f == 0.f ? 1.f : fabsf(f);
-  u32x4 q[KS][T::kQ];
-  {
-    float x[KS][8];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      load8(a.q.p, (int64_t)row * a.q.row + (int64_t)head * a.q.head + g * (DH / 4) + ks * 8, QT, a.q.vec, x[ks]);
-    }
-    if constexpr (CT == PT_F16 && QT == PT_F32) {  // into the range of float16, by a power of two
-      float top = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[ks][i]));
-      top = across_max<16>(top);
-      const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
-      sign = ldexpf(sign, -e);
-      f = ldexpf(f, e);
-    }
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[ks][i] *= sign;
-      split8<CT, T::kQ>(x[ks], q[ks]);
-    }
-  }
+  const int begin = __builtin_amdgcn_readfirstlane((int)min(b0, (int64_t)cap));
+  const int end = __builtin_amdgcn_readfirstlane(split == gr.S - 1 ? kmax : (int)min((int64_t)kmax, b0 + gr.chunk));
 
   f32x4 o[CB];
 #pragma unroll
@@ -573,6 +561,7 @@ __global__ __launch_bounds__(256) void paged_step_kernel(PagedAttend a, Grid gr)
   float m = -INFINITY, l = 0.f;
 
   uint16_t* const vt = reinterpret_cast<uint16_t*>(lds + wave * TILE);
+  constexpr int step = NW * KT;
   u32x4 kr[NB][F4 ? 1 : KS], vr[VU];
   uint32_t ksc[NB], vsc[VU];
   const int32_t* const ids = a.c.pages + (int64_t)s * a.c.max_pages;
@@ -582,21 +571,23 @@ __global__ __launch_bounds__(256) void paged_step_kernel(PagedAttend a, Grid gr)
   // Loads of the block at slot t.  16 slots never cross a page; slots at and behind kmax
   // are read from their page where there is one (any content is masked) and from page 0
   // where not.
-  auto page_at = [&](int t, bool* ok) {
-    const int n = t >> a.c.shift;
-    const int32_t id = ids[min(n, a.c.max_pages - 1)];
-    *ok = t < kmax && (uint32_t)id < (uint32_t)a.c.n_pages;
-    return ((int64_t)(*ok ? id : 0) * a.c.hk + kvh) * a.c.page_bytes;
+  // The ids of a block's pages are fetched one block before its keys, so that no load waits
+  // for the load of its address.
+  int32_t ahead[NB];
+  auto fetch_ids = [&](int t) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) ahead[b] = ids[min((t + 16 * b) >> a.c.shift, a.c.max_pages - 1)];
   };
   auto load = [&](int t) {
     valid = 0;
     int64_t pg[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      bool ok;
-      pg[b] = page_at(t + 16 * b, &ok);
+      const bool ok = t + 16 * b < kmax && (uint32_t)ahead[b] < (uint32_t)a.c.n_pages;
+      pg[b] = ((int64_t)(ok ? ahead[b] : 0) * a.c.hk + kvh) * a.c.page_bytes;
       valid |= (uint32_t)ok << b;
     }
+    fetch_ids(t + step);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const char* kp = a.c.k + pg[b];
@@ -634,41 +625,80 @@ __global__ __launch_bounds__(256) void paged_step_kernel(PagedAttend a, Grid gr)
       if constexpr (F4) vsc[u] = (uint8_t)vp[sc_off + at * PER + lane % PER];
     }
   };
-  const int step = 4 * KT;
   int t = begin + wave * KT;
-  if (t < end) load(t);
+  if (t < end) {
+    fetch_ids(t);
+    load(t);
+  }
+  // queries: channels g DH / 4 + 8 ks .. +7 of row col in step ks
+  float f = a.scale * 1.44269504f;
+  float sign = f < 0.f ? -1.f : f == 0.f ? 0.f : 1.f;
+  f = f == 0.f ? 1.f : fabsf(f);
+  u32x4 q[KS][T::kQ];
+  if constexpr (CT == PT_F16 && QT == PT_F32) {  // into the range of float16, by a power of two
+    float top = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[ks][i]));
+    top = across_max<16>(top);
+    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+    sign = ldexpf(sign, -e);
+    f = ldexpf(f, e);
+  }
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[ks][i] *= sign;
+    split8<CT, T::kQ>(x[ks], q[ks]);
+  }
   for (; t < end; t += step) {
     f32x4 sc[NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      sc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < NB; ++b) sc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        u32x4 kf;
-        if constexpr (F4) kf = decode8(kr[b][0][ks], ksc[b]);
-        else kf = kr[b][ks];
+    for (int ks = 0; ks < KS; ++ks) {
+      u32x4 kf[NB];
 #pragma unroll
-        for (int n = 0; n < T::kQ; ++n) sc[b] = mma16<CT>(kf, q[ks][n], sc[b]);
+      for (int b = 0; b < NB; ++b) {
+        if constexpr (F4) kf[b] = decode8(kr[b][0][ks], ksc[b]);
+        else kf[b] = kr[b][ks];
       }
+#pragma unroll
+      for (int n = 0; n < T::kQ; ++n)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) sc[b] = mma16<CT>(kf[b], q[ks][n], sc[b]);
     }
     const uint32_t ok = valid;
-    // values into the tile; those of slots that no row may see as zeros
+    // blocks that every row sees whole need no mask
     const bool inner = t >= lo_all && t + KT <= hi_all && ok == (1u << NB) - 1;
+    if (!inner) {  // values of slots that no row may see: zeros
+      asm volatile("" ::: "memory");  // a branch, not selects in every block
+#pragma unroll
+      for (int u = 0; u < VU; ++u) {
+        constexpr int PER = F4 ? DH / 32 : DH / 8, ROWS = 64 / PER;
+        const int key = u * ROWS + lane / PER;
+        if (!(t + key >= kmin && t + key < kmax && ((ok >> (key >> 4)) & 1))) {
+          vr[u] = u32x4{0, 0, 0, 0};
+          vsc[u] = 127;
+        }
+      }
+    }
 #pragma unroll
     for (int u = 0; u < VU; ++u) {
       constexpr int PER = F4 ? DH / 32 : DH / 8, ROWS = 64 / PER;
       const int key = u * ROWS + lane / PER;
-      const bool see = inner || (t + key >= kmin && t + key < kmax && ((ok >> (key >> 4)) & 1));
       if constexpr (F4) {
         u32x4* d = reinterpret_cast<u32x4*>(vt + key * PITCH + (lane % PER) * 32);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] = see ? decode8(vr[u][i], vsc[u]) : u32x4{0, 0, 0, 0};
+        for (int i = 0; i < 4; ++i) d[i] = decode8(vr[u][i], vsc[u]);
       } else {
-        *reinterpret_cast<u32x4*>(vt + key * PITCH + (lane % PER) * 8) = see ? vr[u] : u32x4{0, 0, 0, 0};
+        *reinterpret_cast<u32x4*>(vt + key * PITCH + (lane % PER) * 8) = vr[u];
       }
     }
     if (t + step < end) load(t + step);
     if (!inner) {
+      asm volatile("" ::: "memory");
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -683,34 +713,39 @@ __global__ __launch_bounds__(256) void paged_step_kernel(PagedAttend a, Grid gr)
 #pragma unroll
       for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[b][r]);
     mx = across_max<16>(mx);
-    const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn * f;
-    const float alpha = __builtin_amdgcn_exp2f(m * f - ref);
-    m = mn;
-    float ls = 0.f;
+    if (__any(mx * f > fmaf(m, f, kSlack) || m == -INFINITY)) {
+      const float mn = fmaxf(m, mx);
+      const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * f);
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) o[cb] *= alpha;
+    }
+    const float ref = m == -INFINITY ? 0.f : m * f;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         sc[b][r] = __builtin_amdgcn_exp2f(fmaf(sc[b][r], f, -ref));
-        ls += sc[b][r];
+        l += sc[b][r];
       }
-    l = l * alpha + ls;
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) o[cb] *= alpha;
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int b = 0; b < NB; b += 2) {
-      const float x[8] = {sc[b][0], sc[b][1], sc[b][2], sc[b][3], sc[b + 1][0], sc[b + 1][1], sc[b + 1][2], sc[b + 1][3]};
+      const float y[8] = {sc[b][0], sc[b][1], sc[b][2], sc[b][3], sc[b + 1][0], sc[b + 1][1], sc[b + 1][2], sc[b + 1][3]};
       u32x4 p[T::kP];
-      split8<CT, T::kP>(x, p);
+      split8<CT, T::kP>(y, p);
       const uint16_t* src = vt + (16 * b + 4 * g + (col >> 2)) * PITCH + (col & 3) * 4;
+      u32x4 vf[CB];
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
         const uint2 v0 = read_turned(src + cb * 16), v1 = read_turned(src + 16 * PITCH + cb * 16);
-        const u32x4 vf = {v0.x, v0.y, v1.x, v1.y};
-#pragma unroll
-        for (int n = 0; n < T::kP; ++n) o[cb] = mma16<CT>(vf, p[n], o[cb]);
+        vf[cb] = u32x4{v0.x, v0.y, v1.x, v1.y};
       }
+#pragma unroll
+      for (int n = 0; n < T::kP; ++n)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) o[cb] = mma16<CT>(vf[cb], p[n], o[cb]);
     }
     __builtin_amdgcn_wave_barrier();
   }
@@ -719,7 +754,7 @@ __global__ __launch_bounds__(256) void paged_step_kernel(PagedAttend a, Grid gr)
     m = -INFINITY;
     l = 0.f;
   }
-  // join the four waves' states: [wave][query][max, sum, -, -, DH channels]
+  // join the waves' states: [wave][query][max, sum, -, -, DH channels]
   __syncthreads();
   float* const mb = reinterpret_cast<float*>(lds);
   {
@@ -735,14 +770,14 @@ __global__ __launch_bounds__(256) void paged_step_kernel(PagedAttend a, Grid gr)
   // thread: query tid / 16, DH / 16 channels
   constexpr int N = DH / 16;
   const int qj = tid >> 4, c0 = (tid & 15) * N, q2 = tile * 16 + qj;
-  if (q2 >= nq) return;
+  if (tid >= 256 || q2 >= nq) return;
   float mj = -INFINITY, lj = 0.f, oj[N];
 #pragma unroll
-  for (int w = 0; w < 4; ++w) mj = fmaxf(mj, mb[(w * 16 + qj) * (DH + 4)]);
+  for (int w = 0; w < NW; ++w) mj = fmaxf(mj, mb[(w * 16 + qj) * (DH + 4)]);
 #pragma unroll
   for (int i = 0; i < N; ++i) oj[i] = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < NW; ++w) {
     const float* p = mb + (w * 16 + qj) * (DH + 4);
     if (p[0] == -INFINITY && p[1] == 0.f) continue;  // saw nothing
     const float e = __builtin_amdgcn_exp2f(p[0] - mj);
@@ -777,13 +812,9 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
   constexpr int PER = F4 ? DH / 16 : DH / 8, PIECES = KT * PER, NP = PIECES < 256 ? 1 : PIECES / 256;
   __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][KT * PITCH];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
-  int bid = blockIdx.x;
-  const int split = bid % gr.S;
-  bid /= gr.S;
-  const int tile = gr.tiles - 1 - bid % gr.tiles;  // late rows see the most slots: they go first
-  bid /= gr.tiles;
-  const int kvh = bid % a.c.hk, s = bid / a.c.hk;
-  const int G = a.H / a.c.hk;
+  // late rows see the most slots: they go first
+  const int at_x = blockIdx.x / gr.S, tile = gr.tiles - 1 - at_x, split = blockIdx.x - at_x * gr.S, kvh = blockIdx.y, s = blockIdx.z;
+  const int G = gr.G;
   const SeqRows sr = seq_rows(a.r, s);
   const int nq = min(sr.n, a.r.max_rows) * G;
   if (tile * 128 >= nq) return;
@@ -809,8 +840,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
   const int kmin = __builtin_amdgcn_readfirstlane(min(min(ext[0][0], ext[1][0]), min(ext[2][0], ext[3][0])));
   const int kmax = __builtin_amdgcn_readfirstlane(max(max(ext[0][1], ext[1][1]), max(ext[2][1], ext[3][1])));
   const int64_t b0 = (int64_t)(kmin & ~(KT - 1)) + (int64_t)split * gr.chunk;
-  const int begin = (int)min(b0, (int64_t)cap);
-  const int end = split == gr.S - 1 ? kmax : (int)min((int64_t)kmax, b0 + gr.chunk);
+  const int begin = __builtin_amdgcn_readfirstlane((int)min(b0, (int64_t)cap));
+  const int end = __builtin_amdgcn_readfirstlane(split == gr.S - 1 ? kmax : (int)min((int64_t)kmax, b0 + gr.chunk));
 
   float f = a.scale * 1.44269504f;
   float sign = f < 0.f ? -1.f : f == 0.f ? 0.f : 1.f;
@@ -991,12 +1022,14 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
     }
 }
 
-// Joins the splits' sums: one wave per (row, head); lane i looks after split i's state and
-// after DH / 64 channels (a half wave per row for 32).
-template <int DH>
+// Joins the splits' sums, W waves per (row, head): lane i of each looks after split i's
+// state; a wave's lanes take 4 channels each of 256 / DH splits at a time.
+template <int DH, int W>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttend a, int S) {
+  constexpr int LR = DH / 4, P = 64 / LR;  // lanes of a split's row, splits at a time
+  __shared__ float4 part[W == 1 ? 1 : 4][LR];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t i = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t i = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
   const int h = (int)(i % a.H), tok = (int)(i / a.H % a.r.max_rows);
   const int64_t s = i / a.H / a.r.max_rows;
   if (s >= a.c.n_seqs) return;
@@ -1009,27 +1042,33 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttend a, int S) {
   const bool used = !(st.x == -INFINITY && st.y == 0.f);
   const float w = used ? __builtin_amdgcn_exp2f(st.x - m) : 0.f;
   const float l = wave_sum(used ? w * st.y : 0.f);
-  constexpr int N = DH == 128 ? 2 : 1;
-  float o[2] = {0.f, 0.f};
-  const int c0 = (lane * N) & (DH - 1);
-  uint64_t todo = __ballot(used);
-  while (todo != 0) {
-    const int k = __builtin_ctzll(todo);
-    todo &= todo - 1;
-    const float wk = __shfl(w, k);
-    const float* p = a.work + ((int64_t)k * rows + at) * DH + c0;
-#pragma unroll
-    for (int j = 0; j < N; ++j) o[j] += wk * p[j];
+  const int c0 = (lane & (LR - 1)) * 4, first = (W == 1 ? 0 : wave * P) + lane / LR;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int k0 = 0; k0 < S; k0 += (W == 1 ? 1 : 4) * P) {
+    const int k = k0 + first;
+    const float4 p = *reinterpret_cast<const float4*>(a.work + ((int64_t)min(k, S - 1) * rows + at) * DH + c0);
+    const float wk = k < S ? __shfl(w, k) : 0.f;
+    if (wk != 0.f) {  // (a split that saw nothing may hold anything)
+      o.x += wk * p.x; o.y += wk * p.y; o.z += wk * p.z; o.w += wk * p.w;
+    }
   }
+  o.x = across_sum<LR>(o.x); o.y = across_sum<LR>(o.y); o.z = across_sum<LR>(o.z); o.w = across_sum<LR>(o.w);
+  if constexpr (W > 1) {
+    if (lane < LR) part[wave][lane] = o;
+    __syncthreads();
+    if (wave > 0) return;
+    o = part[0][lane & (LR - 1)];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) {
+      const float4 p = part[k][lane & (LR - 1)];
+      o.x += p.x; o.y += p.y; o.z += p.z; o.w += p.w;
+    }
+  }
+  if (lane >= LR) return;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  if (lane * N >= DH) return;
-  const int64_t dst = (int64_t)(sr.row0 + tok) * a.o.row + (int64_t)h * a.o.head + c0;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const float x = l == 0.f ? 0.f : o[j] * inv;
-    if (a.o.type == PT_F32) reinterpret_cast<float*>(a.o.p)[dst + j] = x;
-    else reinterpret_cast<uint16_t*>(a.o.p)[dst + j] = (uint16_t)(a.o.type == PT_BF16 ? pack_bf16(x, 0.f) : pack_f16(x, 0.f));
-  }
+  const float x[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+  store_n(a.o.p, (int64_t)(sr.row0 + tok) * a.o.row + (int64_t)h * a.o.head + c0, a.o.type, a.o.vec, x);
 }
 
 // Few packed rows (rows of a sequence times query heads of a KV head) run on the step
@@ -1040,12 +1079,19 @@ constexpr int kMaxSplits = 64;
 constexpr int kStepBlocks = 1024, kPromptBlocks = 512;
 
 struct Plan {
-  bool step;
+  bool step, wide;
   Grid g;
 };
 
+// Waves of a wide step block: what the registers of a compute unit hold of it.
+constexpr int wide_waves(int type, int dh) { return dh == 128 || type == PT_MXFP4 ? 8 : 16; }
+#ifndef KWIDE
+#define KWIDE 4096
+#endif
+
 Plan plan_of(const PagedCache& c, const PagedRows& r, int H) {
   Plan p;
+  p.g.G = H / c.hk;
   const int64_t packed = (int64_t)r.max_rows * (H / c.hk);
   p.step = packed <= kStepRows;
   const int64_t per = p.step ? 16 : 128;
@@ -1055,6 +1101,8 @@ Plan plan_of(const PagedCache& c, const PagedRows& r, int H) {
   const int64_t want = (p.step ? kStepBlocks : kPromptBlocks) / std::max<int64_t>(blocks, 1);
   int64_t S = std::min<int64_t>(std::min<int64_t>(want, kMaxSplits), (slots + 255) / 256);
   S = std::max<int64_t>(S, 1);
+  p.wide = p.step && S > 1 && slots * c.dh <= KWIDE * 64;
+  if (p.wide) S = 1;
   p.g.chunk = (int)(((slots + S - 1) / S + 63) / 64 * 64);
   p.g.S = (int)((slots + p.g.chunk - 1) / p.g.chunk);
   return p;
@@ -1062,14 +1110,18 @@ Plan plan_of(const PagedCache& c, const PagedRows& r, int H) {
 
 template <int CT, int DH, int QT>
 hipError_t attend_at(const PagedAttend& a, const Plan& p, hipStream_t st, const Ev& ev) {
-  const dim3 grid((uint32_t)((int64_t)p.g.S * p.g.tiles * a.c.hk * a.c.n_seqs));
+  constexpr int NW = wide_waves(CT, DH);
+  const dim3 grid((uint32_t)(p.g.S * p.g.tiles), (uint32_t)a.c.hk, (uint32_t)a.c.n_seqs);
   const bool join = p.g.S > 1;
   hipError_t e;
-  if (p.step) e = plaunch(paged_step_kernel<CT, DH, QT>, grid, dim3(256), st, ev.start, join ? nullptr : ev.stop, a, p.g);
+  if (p.wide) e = plaunch(paged_step_kernel<CT, DH, QT, NW>, grid, dim3(64 * NW), st, ev.start, join ? nullptr : ev.stop, a, p.g);
+  else if (p.step) e = plaunch(paged_step_kernel<CT, DH, QT, 4>, grid, dim3(256), st, ev.start, join ? nullptr : ev.stop, a, p.g);
   else e = plaunch(paged_prompt_kernel<CT, DH, QT>, grid, dim3(256), st, ev.start, join ? nullptr : ev.stop, a, p.g);
   if (e != hipSuccess || !join) return e;
   const int64_t waves = (int64_t)a.c.n_seqs * a.r.max_rows * a.H;
-  return plaunch(paged_join_kernel<DH>, dim3((uint32_t)((waves + 3) / 4)), dim3(256), st, nullptr, ev.stop, a, p.g.S);
+  if (p.g.S <= 256 / DH * 4)
+    return plaunch(paged_join_kernel<DH, 1>, dim3((uint32_t)((waves + 3) / 4)), dim3(256), st, nullptr, ev.stop, a, p.g.S);
+  return plaunch(paged_join_kernel<DH, 4>, dim3((uint32_t)waves), dim3(256), st, nullptr, ev.stop, a, p.g.S);
 }
 
 template <int CT, int DH>

@@ -44,7 +44,7 @@ int check_shape(const mbp_paged_cache* c) {
   if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)) != 0)
     return refuse(MBP_EINVAL, "page_size must be a power of two in [16, 1024]");
   if (c->n_pages < 1) return refuse(MBP_EINVAL, "n_pages must be >= 1");
-  if (c->n_seqs < 0) return refuse(MBP_EINVAL, "n_seqs must be >= 0");
+  if (c->n_seqs < 0 || c->n_seqs > 65535) return refuse(MBP_EINVAL, "n_seqs must be in [0, 65535]");
   if (c->max_pages < 1 || (int64_t)c->max_pages * c->page_size > (1 << 30))
     return refuse(MBP_EINVAL, "max_pages must be >= 1 and max_pages x page_size at most 2^30");
   return MBP_OK;
@@ -213,8 +213,8 @@ int mbp_paged_attend(const mbp_paged_cache* cache, const mbp_paged_rows* rows, i
   if (a.r.n_rows == 0 || a.c.n_seqs == 0 || a.r.max_rows == 0) return MBP_OK;
   const int64_t packed = (int64_t)a.r.max_rows * (n_heads / a.c.hk);
   if (packed > (1 << 30)) return refuse(MBP_ECAPACITY, "max_rows is too large");
-  // the most blocks that any split of the work takes: 64 parts of 16 rows
-  CK(check_grid((int64_t)((packed + 15) / 16) * 64 * a.c.hk * a.c.n_seqs));
+  // the most blocks that any split of a sequence's work takes: 64 parts of 16 rows
+  CK(check_grid((packed + 15) / 16 * 64));
   CK(check_grid((int64_t)a.c.n_seqs * a.r.max_rows * n_heads / 4 + 1));
   const size_t need = paged_work_bytes(a.c, a.r, n_heads);
   if (need > 0 && (d_work == nullptr || !aligned(d_work, 16))) return refuse(MBP_EINVAL, "d_work is null or not aligned to 16 bytes");

@@ -34,17 +34,6 @@ class _Heads(ctypes.Structure):
 
 
 _F32, _BF16, _F16, _MXFP4 = 0, 1, 2, 3  # mbp_dtype
-_numbers = None  # torch dtype -> mbp_dtype
-
-
-def _number(torch, dtype):
-    global _numbers
-    if _numbers is None:
-        _numbers = {torch.float32: _F32, torch.bfloat16: _BF16, torch.float16: _F16}
-    n = _numbers.get(dtype)
-    if n is None:
-        raise ValueError(f"dtype {dtype}: float32, bfloat16 or float16 is needed")
-    return n
 
 
 def declare(L):
@@ -64,7 +53,7 @@ def _ints(torch, name, t, device, n=None):
     """Checks an int32 tensor that the library reads in place; returns its address."""
     if t is None:
         return None
-    if t.dtype is not torch.int32 or t.device != device or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.get_device() != device.index or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous int32 tensor on {device} is needed")
     if n is not None and t.numel() != n:
         raise ValueError(f"{name}: {n} elements are needed, got {t.numel()}")
@@ -85,6 +74,8 @@ class PagedRows:
         import torch
 
         self.device = row_start.device
+        if self.device.type != "cuda":
+            raise ValueError("row_start: a device tensor is needed")
         if first_slot.dim() != 1:
             raise ValueError("first_slot: one dimension is needed")
         self.n_seqs, self.n_rows = first_slot.numel(), int(n_rows)
@@ -130,7 +121,7 @@ class PagedCache:
 
         self.torch, self.L, self.error = torch, lib(), MbpError
         self.device = pages.device
-        if self.device.type != "cuda":
+        if self.device.type != "cuda" or self.device.index is None:
             raise ValueError("pages: a device tensor is needed")
         if pages.dim() != 2:
             raise ValueError("pages: int32 [n_seqs, max_pages] is needed")
@@ -156,18 +147,25 @@ class PagedCache:
         self.k, self.v, self.pages, self.n_seqs = k, v, pages, pages.shape[0]
         self._c.d_k, self._c.d_v = k.data_ptr(), v.data_ptr()
         self._index = self.device.index
+        self._numbers = {torch.float32: _F32, torch.bfloat16: _BF16, torch.float16: _F16}
+        # the stream's address without a Stream object around it, which costs more than a launch
+        self._stream = torch._C._cuda_getCurrentRawStream
         self._single = torch.cuda.device_count() == 1
 
     def _heads(self, name, t, n_rows, heads=None):
-        if t.dim() != 3 or t.shape[0] != n_rows or t.shape[2] != self.d_head or (heads is not None and t.shape[1] != heads):
-            raise ValueError(f"{name}: [{n_rows}, {'heads' if heads is None else heads}, {self.d_head}] is needed, got {list(t.shape)}")
-        if t.device != self.device:
+        shape = t.shape
+        if len(shape) != 3 or shape[0] != n_rows or shape[2] != self.d_head or (heads is not None and shape[1] != heads):
+            raise ValueError(f"{name}: [{n_rows}, {'heads' if heads is None else heads}, {self.d_head}] is needed, got {list(shape)}")
+        if t.get_device() != self._index:
             raise ValueError(f"{name} is on {t.device}, the cache on {self.device}")
         rs, hs, es = t.stride()
         if es != 1:
             raise ValueError(f"{name}: the channels of a head must be adjacent")
+        number = self._numbers.get(t.dtype)
+        if number is None:
+            raise ValueError(f"{name}: float32, bfloat16 or float16 is needed, got {t.dtype}")
         # a tensor without elements has no address: one that is never followed stands in
-        return _Heads(t.data_ptr() or 16, _number(self.torch, t.dtype), rs, hs)
+        return _Heads(t.data_ptr() or 16, number, rs, hs)
 
     def _check_rows(self, rows):
         if rows.n_seqs != self.n_seqs or rows.device != self.device:
@@ -175,12 +173,11 @@ class PagedCache:
 
     def _run(self, fn, *args):
         """The call on the cache's device and its current stream."""
-        cuda = self.torch.cuda
-        stream = cuda.current_stream(self.device).cuda_stream
-        if self._single or cuda.current_device() == self._index:
+        stream = self._stream(self._index)
+        if self._single or self.torch.cuda.current_device() == self._index:
             rc = fn(*args, stream)
         else:
-            with cuda.device(self.device):
+            with self.torch.cuda.device(self.device):
                 rc = fn(*args, stream)
         if rc:
             raise self.error(rc, self.L.mbp_paged_error().decode())
