@@ -58,8 +58,8 @@ struct PagedAttend {
   const int32_t* lo;  // first visible slot of each row, or nullptr: 0
   const int32_t* hi;  // end of the visible slots, or nullptr: the row's slot + 1
   float scale;
-  // split sums (paged_work_bytes): [splits][n_rows][H] rows of dh floats, then as many
-  // (max, sum) pairs
+  // split sums (paged_work_bytes): [splits][n_seqs][max_rows][H] rows of dh floats, then as
+  // many (max, sum) pairs
   float* work;
 };
 

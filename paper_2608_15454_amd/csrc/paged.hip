@@ -43,34 +43,48 @@ __device__ __forceinline__ float hi_bf16(uint32_t u) { return __uint_as_float(u 
 __device__ __forceinline__ float lo_f16(uint32_t u) { return (float)__builtin_bit_cast(f16x2, u)[0]; }
 __device__ __forceinline__ float hi_f16(uint32_t u) { return (float)__builtin_bit_cast(f16x2, u)[1]; }
 
-// Elements [at, at + 8) of rows of type t.
-__device__ __forceinline__ void load8(const void* p, int64_t at, int t, int vec, float (&x)[8]) {
-  if (t == PT_F32) {
-    const float* f = reinterpret_cast<const float*>(p) + at;
-    if (vec) {
-      const float4 a = *reinterpret_cast<const float4*>(f), b = *reinterpret_cast<const float4*>(f + 4);
-      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-      x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = f[i];
-    }
+// Elements [at, at + 8) of rows of type t as they lie in memory (16-bit types: in u[0]),
+// and their values: apart, so that several can be in flight.
+struct Raw8 {
+  uint4 u[2];
+};
+__device__ __forceinline__ void load_raw8(const void* p, int64_t at, int t, int vec, Raw8& r) {
+  if (vec) {
+    const char* c = reinterpret_cast<const char*>(p) + at * (t == PT_F32 ? 4 : 2);
+    r.u[0] = *reinterpret_cast<const uint4*>(c);
+    if (t == PT_F32) r.u[1] = *reinterpret_cast<const uint4*>(c + 16);
     return;
   }
-  const uint16_t* h = reinterpret_cast<const uint16_t*>(p) + at;
-  uint32_t u[4];
-  if (vec) {
-    const uint4 a = *reinterpret_cast<const uint4*>(h);
-    u[0] = a.x; u[1] = a.y; u[2] = a.z; u[3] = a.w;
-  } else {
+  uint32_t w[8];
+  if (t == PT_F32) {
+    const uint32_t* f = reinterpret_cast<const uint32_t*>(p) + at;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = (uint32_t)h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
+    for (int i = 0; i < 8; ++i) w[i] = f[i];
+    r.u[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  } else {
+    const uint16_t* h = reinterpret_cast<const uint16_t*>(p) + at;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
+  }
+  r.u[0] = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void values8(const Raw8& r, int t, float (&x)[8]) {
+  const uint32_t w[8] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w, r.u[1].x, r.u[1].y, r.u[1].z, r.u[1].w};
+  if (t == PT_F32) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+    return;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    x[2 * i] = t == PT_BF16 ? lo_bf16(u[i]) : lo_f16(u[i]);
-    x[2 * i + 1] = t == PT_BF16 ? hi_bf16(u[i]) : hi_f16(u[i]);
+    x[2 * i] = t == PT_BF16 ? lo_bf16(w[i]) : lo_f16(w[i]);
+    x[2 * i + 1] = t == PT_BF16 ? hi_bf16(w[i]) : hi_f16(w[i]);
   }
+}
+__device__ __forceinline__ void load8(const void* p, int64_t at, int t, int vec, float (&x)[8]) {
+  Raw8 r;
+  load_raw8(p, at, t, vec, r);
+  values8(r, t, x);
 }
 
 template <int N>
@@ -117,16 +131,73 @@ __device__ __forceinline__ SeqRows seq_rows(const PagedRows& r, int s) {
   return {a, b - a, r.first_slot[s]};
 }
 
-// The sequence that holds row `row`, or -1: the last one that begins at or before it.  A
-// wave looks through 64 starts at a time; row is the same in all its lanes.
-__device__ __forceinline__ int seq_of(const PagedRows& r, int n_seqs, int row) {
+// The sequence that begins last at or before a row (which may lie behind its end), its
+// rows and the slot of the first; s = -1: none does.
+struct RowSeq {
+  int32_t s, start, end, slot0;
+};
+
+// Of a row that all lanes of the wave agree on.  A wave looks through 64 sequences at a
+// time, and their starts, ends and slots are loaded together: one load's latency, where a
+// binary search would have one for each step.
+__device__ __forceinline__ RowSeq seq_of(const PagedRows& r, int n_seqs, int row) {
   const int lane = threadIdx.x & 63;
-  int s = -1;
+  RowSeq f = {-1, 0, 0, 0};
   for (int at = 0; at < n_seqs; at += 64) {
-    const int i = at + lane;
-    s += (int)__popcll(__ballot(i < n_seqs && r.row_start[min(i, n_seqs)] <= row));
+    const int i = min(at + lane, n_seqs - 1);
+    const int32_t start = r.row_start[i], end = r.row_start[i + 1], slot0 = r.first_slot[i];
+    const int n = (int)__popcll(__ballot(at + lane < n_seqs && start <= row));
+    if (n > 0) {
+      f.s = at + n - 1;
+      f.start = __builtin_amdgcn_readlane(start, n - 1);
+      f.end = __builtin_amdgcn_readlane(end, n - 1);
+      f.slot0 = __builtin_amdgcn_readlane(slot0, n - 1);
+    }
   }
-  return s;
+  return f;
+}
+
+// On to the sequence of a later row.
+__device__ __forceinline__ void advance(const PagedRows& r, int n_seqs, int row, RowSeq* f) {
+  while (row >= f->end && f->s + 1 < n_seqs && r.row_start[f->s + 1] <= row) {
+    ++f->s;
+    f->start = r.row_start[f->s];
+    f->end = r.row_start[f->s + 1];
+    f->slot0 = r.first_slot[f->s];
+  }
+}
+
+// The slot of a row, -1 for one of no sequence.
+__device__ __forceinline__ int32_t slot_of(const RowSeq& f, int row) {
+  if (f.s < 0 || row < f.start || row >= f.end) return -1;
+  return (int32_t)min(max((int64_t)f.slot0 + (row - max(f.start, 0)), (int64_t)-1), (int64_t)INT32_MAX);
+}
+
+// A wave's part of a call on token rows: 64 units of 8 channels each of the heads of one
+// kind (queries, keys or values), in `rows` rows one after the other.  What belongs to a
+// row (its sequence, slot, page, position) is then the same in all lanes and costs scalar
+// instructions, what belongs to a lane (its head and channel) stays from row to row, and
+// the slots that a wave writes lie side by side.
+struct Tasks {
+  int32_t first[3], chunks;  // chunks of 64 units before each kind, and of all
+  int32_t per_shift;         // log2 of the units of a head
+  int32_t rows;
+};
+struct Lane {
+  int32_t which, h, c0, row0;
+  bool live;
+};
+__device__ __forceinline__ Lane lane_of(const Tasks& tk, int heads0, int heads) {
+  const int id = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int group = id / tk.chunks, chunk = id - group * tk.chunks;
+  Lane l;
+  l.which = chunk < tk.first[1] ? 0 : chunk < tk.first[2] ? 1 : 2;
+  const int unit = (chunk - tk.first[l.which]) * 64 + ((int)threadIdx.x & 63);
+  l.h = unit >> tk.per_shift;
+  l.c0 = (unit & ((1 << tk.per_shift) - 1)) * 8;
+  l.live = l.h < (l.which == 0 ? heads0 : heads);
+  l.row0 = group * tk.rows;
+  return l;
 }
 
 // Byte offset of slot 0 of a page of head h, or -1 where the slot has no page.
@@ -159,6 +230,17 @@ __device__ __forceinline__ uint32_t codes8(const float (&y)[8]) {
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[6], y[7], 1.0f, 3);
 }
 
+// 8 codes of one scale block as bfloat16.
+__device__ __forceinline__ u32x4 decode8(uint32_t u, uint32_t scale_byte) {
+  const float sc = __uint_as_float(scale_byte << 23);
+  u32x4 r;
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 0));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 1));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 2));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 3));
+  return r;
+}
+
 // d as float32 whose last bit says whether something was cut off (round to odd): rounding
 // that again to fewer bits gives what rounding d would give.
 __device__ __forceinline__ float round_odd(double d) {
@@ -173,158 +255,167 @@ __device__ __forceinline__ float round_odd(double d) {
 }
 
 // ------------------------------------------------------------------- append ----
-// A thread takes 8 channels of one head of one row, the heads of a row in the order q, k,
-// v; 4 neighbouring threads share a scale block of 32.  Every value is read once and
-// written once, so the copy rate bounds it; the rotation is three operations a channel.
-template <int CT>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, int units_row, int64_t units) {
-  const int64_t u0 = (int64_t)blockIdx.x * 256;
-  const int row0 = (int)(u0 / units_row);
-  int s = seq_of(a.r, a.c.n_seqs, row0);
-  // units past the block's first row: the quotient is small, float32 has it exactly but
-  // for the last unit, which the comparisons put right
-  int unit = (int)(u0 - (int64_t)row0 * units_row) + threadIdx.x;
-  int off = (int)((float)unit / (float)units_row);
-  off += unit - off * units_row >= units_row;
-  off -= unit - off * units_row < 0;
-  unit -= off * units_row;
-  const int row = row0 + off;
-  if (u0 + threadIdx.x >= units) return;
-  while (s + 1 < a.c.n_seqs && a.r.row_start[s + 1] <= row) ++s;
-  if (s < 0) return;
-  const SeqRows sr = seq_rows(a.r, s);
-  if (row < sr.row0 || row >= sr.row0 + sr.n) return;
-  const int32_t slot = (int32_t)min((int64_t)sr.slot0 + (row - sr.row0), (int64_t)INT32_MAX);
-  const int dh = a.c.dh, per = dh >> 3;
-  const int nq = a.q.p != nullptr ? a.H : 0;
-  int h = unit / per;
-  const int c0 = (unit - h * per) * 8;
-  const int which = h < nq ? 0 : h < nq + a.c.hk ? 1 : 2;
-  h -= which == 0 ? 0 : which == 1 ? nq : nq + a.c.hk;
-  float x[8];
-  const HeadRows& src = which == 0 ? a.q : which == 1 ? a.k : a.v;
-  float4 cs[4];
-  const bool turn = which < 2 && a.rope != nullptr;
-  if (turn) {
-    const int32_t pos = a.pos != nullptr ? a.pos[row] : slot;
-    if ((uint32_t)pos >= (uint32_t)a.n_pos) return;
-    const float4* t = reinterpret_cast<const float4*>(a.rope + ((int64_t)pos * dh + c0) / 2);
-    cs[0] = t[0];
-    cs[1] = t[1];
-  } else if (a.rope != nullptr && a.pos != nullptr) {
-    if ((uint32_t)a.pos[row] >= (uint32_t)a.n_pos) return;
-  } else if (a.rope != nullptr && (uint32_t)slot >= (uint32_t)a.n_pos) {
-    return;
-  }
-  load8(src.p, (int64_t)row * src.row + (int64_t)h * src.head + c0, src.type, src.vec, x);
-  if (which == 0 || CT != PT_MXFP4) {
-    if (turn) {
+// Every value is read once and written once, so the copy rate bounds it; the rotation is
+// three operations a channel.  U rows' loads are in flight together.
+template <int CT, int U>
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, Tasks tk) {
+  const Lane l = lane_of(tk, a.H, a.c.hk);
+  const int dh = a.c.dh;
+  if (l.row0 >= a.r.n_rows) return;
+  RowSeq f = seq_of(a.r, a.c.n_seqs, l.row0);
+  const HeadRows src = l.which == 0 ? a.q : l.which == 1 ? a.k : a.v;
+  const bool turn = l.which < 2 && a.rope != nullptr;
+  const int64_t at_src = (int64_t)l.h * src.head + l.c0, at_out = (int64_t)l.h * a.qo.head + l.c0;
+  const int64_t head = (int64_t)l.h * a.c.page_bytes;
+  char* const pool = l.which == 1 ? a.c.k : a.c.v;
+  const int es = src.type == PT_F32 ? 4 : 2;
+  const int last = min(l.row0 + tk.rows, a.r.n_rows);
+  Raw8 raw[U];
+  float4 cs[U][2];
+  int32_t slot[U], id[U];
+  bool ok[U];
+  auto fetch = [&](int row, int j) {
+    advance(a.r, a.c.n_seqs, row, &f);
+    slot[j] = slot_of(f, row);
+    ok[j] = row < last && f.s >= 0 && row >= f.start && row < f.end;
+    int32_t pos = slot[j];
+    if (a.rope != nullptr) {
+      if (a.pos != nullptr) pos = a.pos[min(row, a.r.n_rows - 1)];
+      ok[j] = ok[j] && (uint32_t)pos < (uint32_t)a.n_pos;
+    }
+    id[j] = -1;
+    if (l.which > 0 && slot[j] >= 0 && (slot[j] >> a.c.shift) < a.c.max_pages)
+      id[j] = a.c.pages[(int64_t)f.s * a.c.max_pages + (slot[j] >> a.c.shift)];
+    if (!ok[j]) return;
+    if (l.live) {
+      load_raw8(reinterpret_cast<const char*>(src.p) + (int64_t)row * src.row * es, at_src, src.type, src.vec, raw[j]);
+      if (turn) {
+        const float4* t = reinterpret_cast<const float4*>(a.rope + (int64_t)pos * (dh / 2)) + l.c0 / 4;
+        cs[j][0] = t[0];
+        cs[j][1] = t[1];
+      }
+    }
+  };
+  auto put = [&](int row, int j) {
+    float x[8];
+    values8(raw[j], src.type, x);
+    if ((l.which == 0 || CT != PT_MXFP4) && turn) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float c = i & 1 ? cs[i >> 1].z : cs[i >> 1].x, sn = i & 1 ? cs[i >> 1].w : cs[i >> 1].y;
+        const float c = i & 1 ? cs[j][i >> 1].z : cs[j][i >> 1].x, sn = i & 1 ? cs[j][i >> 1].w : cs[j][i >> 1].y;
         const float r0 = x[2 * i] * c - x[2 * i + 1] * sn, r1 = x[2 * i] * sn + x[2 * i + 1] * c;
         x[2 * i] = r0;
         x[2 * i + 1] = r1;
       }
     }
-    if (which == 0) {
-      store_n(a.qo.p, (int64_t)row * a.qo.row + (int64_t)h * a.qo.head + c0, a.qo.type, a.qo.vec, x);
+    if (l.which == 0) {
+      store_n(reinterpret_cast<char*>(a.qo.p) + (int64_t)row * a.qo.row * es, at_out, a.qo.type, a.qo.vec, x);
       return;
     }
-  }
-  const int64_t page = page_of(a.c, s, slot, h);
-  if (page < 0) return;
-  char* pool = (which == 1 ? a.c.k : a.c.v) + page;
-  const int at = slot & ((1 << a.c.shift) - 1);
-  if constexpr (CT != PT_MXFP4) {
-    if constexpr (CT == PT_F16) {  // finite values beyond the type's largest are held as that
+    if ((uint32_t)id[j] >= (uint32_t)a.c.n_pages) return;
+    char* page = pool + (int64_t)id[j] * a.c.hk * a.c.page_bytes + head;
+    const int at = slot[j] & ((1 << a.c.shift) - 1);
+    if constexpr (CT != PT_MXFP4) {
+      if constexpr (CT == PT_F16) {  // finite values beyond the type's largest are held as that
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = fabsf(x[i]) < INFINITY ? fminf(fmaxf(x[i], -65504.f), 65504.f) : x[i];
-    }
-    store_n(pool, (int64_t)at * dh + c0, CT, 1, x);
-  } else {
-    // A value beside the middle of two codes has to go to the right one, and so has the
-    // largest value beside a power of two: keys are rotated in float64, where the products
-    // are exact, and reach the conversion through a float32 that is rounded to odd.
-    float y[8];
-    int byte;
-    if (turn) {
-      double d[8];
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const double c = i & 1 ? cs[i >> 1].z : cs[i >> 1].x, sn = i & 1 ? cs[i >> 1].w : cs[i >> 1].y;
-        d[2 * i] = (double)x[2 * i] * c - (double)x[2 * i + 1] * sn;
-        d[2 * i + 1] = (double)x[2 * i] * sn + (double)x[2 * i + 1] * c;
+        for (int i = 0; i < 8; ++i) x[i] = fabsf(x[i]) < INFINITY ? fminf(fmaxf(x[i], -65504.f), 65504.f) : x[i];
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, (uint32_t)(__builtin_bit_cast(uint64_t, d[i]) >> 32) & 0x7fffffffu);
-      byte = scale_byte((int)(quad_max(top) >> 20), 2047);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = round_odd(ldexp(d[i], 127 - byte));
+      store_n(page, at * dh + l.c0, CT, 1, x);
     } else {
-      uint32_t top = 0;
+      // A value beside the middle of two codes has to go to the right one, and so has the
+      // largest value beside a power of two: keys are rotated in float64, where the products
+      // are exact, and reach the conversion through a float32 that is rounded to odd.
+      float y[8];
+      int byte;
+      if (turn) {
+        double d[8];
+        uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-      byte = scale_byte((int)(quad_max(top) >> 23), 255);
+        for (int i = 0; i < 4; ++i) {
+          const double c = i & 1 ? cs[j][i >> 1].z : cs[j][i >> 1].x, sn = i & 1 ? cs[j][i >> 1].w : cs[j][i >> 1].y;
+          d[2 * i] = (double)x[2 * i] * c - (double)x[2 * i + 1] * sn;
+          d[2 * i + 1] = (double)x[2 * i] * sn + (double)x[2 * i + 1] * c;
+        }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = ldexpf(x[i], 127 - byte);
+        for (int i = 0; i < 8; ++i) top = max(top, (uint32_t)(__builtin_bit_cast(uint64_t, d[i]) >> 32) & 0x7fffffffu);
+        byte = scale_byte((int)(quad_max(top) >> 20), 2047);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = round_odd(ldexp(d[i], 127 - byte));
+      } else {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+        byte = scale_byte((int)(quad_max(top) >> 23), 255);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = ldexpf(x[i], 127 - byte);
+      }
+      const uint32_t u = byte == 255 ? 0u : codes8(y);
+      *reinterpret_cast<uint32_t*>(page + (at * dh + l.c0) / 2) = u;
+      if ((l.c0 & 31) == 0) page[(dh / 2 << a.c.shift) + at * (dh >> 5) + (l.c0 >> 5)] = (char)byte;
     }
-    const uint32_t u = byte == 255 ? 0u : codes8(y);
-    *reinterpret_cast<uint32_t*>(pool + (at * dh + c0) / 2) = u;
-    if ((c0 & 31) == 0) pool[(dh / 2 << a.c.shift) + at * (dh >> 5) + (c0 >> 5)] = (char)byte;
+  };
+  for (int row = l.row0; row < last; row += U) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) fetch(row + j, j);
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (ok[j] && l.live) put(row + j, j);
   }
 }
 
 // --------------------------------------------------------------------- read ----
-__global__ __launch_bounds__(256) void paged_read_kernel(PagedCache c, PagedRows r, HeadRows ko, HeadRows vo, int units_row,
-                                                         int64_t units) {
-  const int64_t u0 = (int64_t)blockIdx.x * 256;
-  const int row0 = (int)(u0 / units_row);
-  int s = seq_of(r, c.n_seqs, row0);
-  int unit = (int)(u0 - (int64_t)row0 * units_row) + threadIdx.x;
-  int off = (int)((float)unit / (float)units_row);
-  off += unit - off * units_row >= units_row;
-  off -= unit - off * units_row < 0;
-  unit -= off * units_row;
-  const int row = row0 + off;
-  if (u0 + threadIdx.x >= units) return;
-  while (s + 1 < c.n_seqs && r.row_start[s + 1] <= row) ++s;
-  int32_t slot = -1;  // of no sequence: nothing there
-  if (s >= 0) {
-    const SeqRows sr = seq_rows(r, s);
-    if (row >= sr.row0 && row < sr.row0 + sr.n) slot = (int32_t)min((int64_t)sr.slot0 + (row - sr.row0), (int64_t)INT32_MAX);
-  }
-  const int dh = c.dh, per = dh >> 3;
-  int h = unit / per;
-  const int c0 = (unit - h * per) * 8;
-  const bool val = h >= c.hk;
-  h -= val ? c.hk : 0;
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  const int64_t page = page_of(c, s, slot, h);
-  if (page >= 0) {
-    const char* pool = (val ? c.v : c.k) + page;
+template <int CT, int U>
+__global__ __launch_bounds__(256) void paged_read_kernel(PagedCache c, PagedRows r, HeadRows ko, HeadRows vo, Tasks tk) {
+  const Lane l = lane_of(tk, 0, c.hk);
+  const int dh = c.dh;
+  if (l.row0 >= r.n_rows) return;
+  RowSeq f = seq_of(r, c.n_seqs, l.row0);
+  const HeadRows dst = l.which == 1 ? ko : vo;
+  const char* const pool = l.which == 1 ? c.k : c.v;
+  const int64_t at_dst = (int64_t)l.h * dst.head + l.c0, head = (int64_t)l.h * c.page_bytes;
+  const int es = dst.type == PT_F32 ? 4 : 2;
+  const int last = min(l.row0 + tk.rows, r.n_rows);
+  u32x4 raw[U];
+  uint32_t byte[U];
+  auto fetch = [&](int row, int j) {
+    raw[j] = u32x4{0, 0, 0, 0};
+    byte[j] = 127;
+    if (row >= last) return;
+    advance(r, c.n_seqs, row, &f);
+    const int32_t slot = slot_of(f, row);
+    if (slot < 0 || (slot >> c.shift) >= c.max_pages) return;
+    const int32_t id = c.pages[(int64_t)f.s * c.max_pages + (slot >> c.shift)];
+    if ((uint32_t)id >= (uint32_t)c.n_pages || !l.live) return;
+    const char* page = pool + (int64_t)id * c.hk * c.page_bytes + head;
     const int at = slot & ((1 << c.shift) - 1);
-    if (c.type != PT_MXFP4) {
-      load8(pool, (int64_t)at * dh + c0, c.type, 1, x);
+    if constexpr (CT != PT_MXFP4) {
+      raw[j] = *reinterpret_cast<const u32x4*>(page + (at * dh + l.c0) * 2);
     } else {
-      const uint32_t u = *reinterpret_cast<const uint32_t*>(pool + (at * dh + c0) / 2);
-      const float sc = __uint_as_float((uint32_t)(uint8_t)pool[(dh / 2 << c.shift) + at * (dh >> 5) + (c0 >> 5)] << 23);
-      const bf16x2_t b[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 1),
-                             __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 3)};
+      raw[j][0] = *reinterpret_cast<const uint32_t*>(page + (at * dh + l.c0) / 2);
+      byte[j] = (uint8_t)page[(dh / 2 << c.shift) + at * (dh >> 5) + (l.c0 >> 5)];
+    }
+  };
+  for (int row = l.row0; row < last; row += U) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) fetch(row + j, j);
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      if (row + j >= last || !l.live) continue;
+      u32x4 u = raw[j];
+      if constexpr (CT == PT_MXFP4) u = decode8(raw[j][0], byte[j]);
+      float x[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[2 * i] = lo_bf16(__builtin_bit_cast(uint32_t, b[i]));
-        x[2 * i + 1] = hi_bf16(__builtin_bit_cast(uint32_t, b[i]));
+        x[2 * i] = CT == PT_F16 ? lo_f16(u[i]) : lo_bf16(u[i]);
+        x[2 * i + 1] = CT == PT_F16 ? hi_f16(u[i]) : hi_bf16(u[i]);
       }
+      if (CT != PT_F16 && dst.type == PT_F16) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = fabsf(x[i]) < INFINITY ? fminf(fmaxf(x[i], -65504.f), 65504.f) : x[i];
+      }
+      store_n(reinterpret_cast<char*>(dst.p) + (int64_t)(row + j) * dst.row * es, at_dst, dst.type, dst.vec, x);
     }
   }
-  const HeadRows& dst = val ? vo : ko;
-  if (dst.type == PT_F16) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = fabsf(x[i]) < INFINITY ? fminf(fmaxf(x[i], -65504.f), 65504.f) : x[i];
-  }
-  store_n(dst.p, (int64_t)row * dst.row + (int64_t)h * dst.head + c0, dst.type, dst.vec, x);
 }
 
 // ------------------------------------------------------------------- attend ----
@@ -391,17 +482,6 @@ __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// 8 codes of one scale block as bfloat16.
-__device__ __forceinline__ u32x4 decode8(uint32_t u, uint32_t scale_byte) {
-  const float sc = __uint_as_float(scale_byte << 23);
-  u32x4 r;
-  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 0));
-  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 1));
-  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 2));
-  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 3));
-  return r;
 }
 
 // The 4 x 16 tile of 16-bit values that the 16 lanes of a quarter wave point at (lane i:
@@ -490,10 +570,11 @@ struct Grid {  // of an attention launch: x is split fastest, then tile; y the K
 // terms far from the type's ends.
 constexpr float kSlack = 8.f;
 
-// Where a row's channels go: the output, or this split's sums.
+// Where a row's channels go: the output, or this split's sums, at place `place` (its
+// sequence's place times max_rows, plus the row's in that: known without a load).
 template <int N>
-__device__ __forceinline__ void put_out(const PagedAttend& a, int S, int split, int row, int head, int dh, int c0, float m, float l,
-                                        float (&o)[N]) {
+__device__ __forceinline__ void put_out(const PagedAttend& a, int S, int split, int64_t place, int row, int head, int dh, int c0,
+                                        float m, float l, float (&o)[N]) {
   if (S == 1) {
     const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
@@ -501,7 +582,7 @@ __device__ __forceinline__ void put_out(const PagedAttend& a, int S, int split, 
     store_n(a.o.p, (int64_t)row * a.o.row + (int64_t)head * a.o.head + c0, a.o.type, a.o.vec, o);
     return;
   }
-  const int64_t i = ((int64_t)split * a.r.n_rows + row) * a.H + head, all = (int64_t)S * a.r.n_rows * a.H;
+  const int64_t rows = (int64_t)a.c.n_seqs * a.r.max_rows, i = ((int64_t)split * rows + place) * a.H + head, all = S * rows * a.H;
   store_n(a.work, i * dh + c0, PT_F32, 1, o);
   if (c0 == 0) reinterpret_cast<float2*>(a.work + all * dh)[i] = make_float2(m, l);
 }
@@ -537,10 +618,21 @@ __global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_ke
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int tile = gr.tiles == 1 ? 0 : blockIdx.x / gr.S, split = blockIdx.x - tile * gr.S, kvh = blockIdx.y, s = blockIdx.z;
   const int G = gr.G;
+  const int cap = a.c.max_pages << a.c.shift;
+  const int32_t* const ids = a.c.pages + (int64_t)s * a.c.max_pages;
+  // The ids of a block's pages are fetched one block before its keys, so that no load waits
+  // for the load of its address.
+  int32_t ahead[NB];
+  auto fetch_ids = [&](int t) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) ahead[b] = ids[min((t + 16 * b) >> a.c.shift, a.c.max_pages - 1)];
+  };
+  // without lower ends the split's first slots are known at once, and their pages' ids are
+  // loaded beside the sequence's rows
+  fetch_ids(a.lo == nullptr ? (int)min((int64_t)split * gr.chunk, (int64_t)cap) + wave * KT : 0);
   const SeqRows sr = seq_rows(a.r, s);
   const int nq = min(sr.n, a.r.max_rows) * G;
   if (tile * 16 >= nq) return;
-  const int cap = a.c.max_pages << a.c.shift;
   const int qi = tile * 16 + col, tok = G == 1 ? min(qi, nq - 1) : min(qi, nq - 1) / G,
             head = kvh * G + min(qi, nq - 1) - tok * G, row = sr.row0 + tok;
   float x[KS][8];
@@ -549,7 +641,7 @@ __global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_ke
     load8(a.q.p, (int64_t)row * a.q.row + (int64_t)head * a.q.head + g * (DH / 4) + ks * 8, QT, a.q.vec, x[ks]);
   int lo = cap, hi = 0;
   if (qi < nq) row_range(a, sr, tok, cap, &lo, &hi);
-  const int kmin = __builtin_amdgcn_readfirstlane(min16(lo)), kmax = __builtin_amdgcn_readfirstlane(max16(hi));
+  const int kmin = a.lo == nullptr ? 0 : __builtin_amdgcn_readfirstlane(min16(lo)), kmax = __builtin_amdgcn_readfirstlane(max16(hi));
   const int lo_all = __builtin_amdgcn_readfirstlane(max16(hi > 0 ? lo : 0)), hi_all = __builtin_amdgcn_readfirstlane(min16(hi > 0 ? hi : cap));
   const int64_t b0 = (int64_t)(kmin & ~(KT - 1)) + (int64_t)split * gr.chunk;
   const int begin = __builtin_amdgcn_readfirstlane((int)min(b0, (int64_t)cap));
@@ -564,20 +656,12 @@ __global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_ke
   constexpr int step = NW * KT;
   u32x4 kr[NB][F4 ? 1 : KS], vr[VU];
   uint32_t ksc[NB], vsc[VU];
-  const int32_t* const ids = a.c.pages + (int64_t)s * a.c.max_pages;
   const uint32_t in_page = (1u << a.c.shift) - 1;
   const int sc_off = DH / 2 << a.c.shift;
   uint32_t valid = 0;  // of the block whose keys are in the registers: a bit for each 16 slots
   // Loads of the block at slot t.  16 slots never cross a page; slots at and behind kmax
   // are read from their page where there is one (any content is masked) and from page 0
   // where not.
-  // The ids of a block's pages are fetched one block before its keys, so that no load waits
-  // for the load of its address.
-  int32_t ahead[NB];
-  auto fetch_ids = [&](int t) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b) ahead[b] = ids[min((t + 16 * b) >> a.c.shift, a.c.max_pages - 1)];
-  };
   auto load = [&](int t) {
     valid = 0;
     int64_t pg[NB];
@@ -626,10 +710,8 @@ __global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_ke
     }
   };
   int t = begin + wave * KT;
-  if (t < end) {
-    fetch_ids(t);
-    load(t);
-  }
+  if (a.lo != nullptr) fetch_ids(t);
+  if (t < end) load(t);
   // queries: channels g DH / 4 + 8 ks .. +7 of row col in step ks
   float f = a.scale * 1.44269504f;
   float sign = f < 0.f ? -1.f : f == 0.f ? 0.f : 1.f;
@@ -794,7 +876,7 @@ __global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_ke
     row_range(a, sr, tok2, cap, &lo2, &hi2);
     sum_values<CT, DH>(a, s, kvh, sr.row0 + tok2, head2, max(lo2, begin), min(hi2, end), mj, a.scale * 1.44269504f, c0, oj);
   }
-  put_out(a, gr.S, split, sr.row0 + tok2, head2, DH, c0, mj, lj, oj);
+  put_out(a, gr.S, split, (int64_t)s * a.r.max_rows + tok2, sr.row0 + tok2, head2, DH, c0, mj, lj, oj);
 }
 
 // Many query rows: 128 per block (32 per wave, lane l owning query l % 32) against the
@@ -1018,7 +1100,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
       const bool odd = !(fabsf(x[0]) < INFINITY && fabsf(x[1]) < INFINITY && fabsf(x[2]) < INFINITY && fabsf(x[3]) < INFINITY);
       if (odd && l < INFINITY)
         sum_values<CT, DH>(a, s, kvh, row, head, max(lo, begin), min(hi, end), m, a.scale * 1.44269504f, c0, x);
-      put_out(a, gr.S, split, row, head, DH, c0, m, l, x);
+      put_out(a, gr.S, split, (int64_t)s * a.r.max_rows + tok, row, head, DH, c0, m, l, x);
     }
 }
 
@@ -1029,28 +1111,38 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttend a, int S) {
   constexpr int LR = DH / 4, P = 64 / LR;  // lanes of a split's row, splits at a time
   __shared__ float4 part[W == 1 ? 1 : 4][LR];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t i = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
-  const int h = (int)(i % a.H), tok = (int)(i / a.H % a.r.max_rows);
-  const int64_t s = i / a.H / a.r.max_rows;
-  if (s >= a.c.n_seqs) return;
-  const SeqRows sr = seq_rows(a.r, (int)s);
-  if (tok >= sr.n) return;
-  const int64_t rows = (int64_t)a.r.n_rows * a.H, at = (int64_t)(sr.row0 + tok) * a.H + h;
+  const int64_t at = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;  // place of the row times heads, plus head
+  const int64_t rows = (int64_t)a.c.n_seqs * a.r.max_rows * a.H;
+  if (at >= rows) return;
+  // everything that the sums take is loaded at once; rows that do not exist read what the
+  // workspace holds, and write nothing
   const float2* ml = reinterpret_cast<const float2*>(a.work + rows * S * DH);
-  const float2 st = lane < S ? ml[lane * rows + at] : make_float2(-INFINITY, 0.f);
+  float2 st = ml[min(lane, S - 1) * rows + at];
+  if (lane >= S) st = make_float2(-INFINITY, 0.f);
+  const int c0 = (lane & (LR - 1)) * 4, first = (W == 1 ? 0 : wave * P) + lane / LR;
+  constexpr int STEP = (W == 1 ? 1 : 4) * P, AHEAD = 4;
+  float4 p[AHEAD];
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j)
+    p[j] = *reinterpret_cast<const float4*>(a.work + ((int64_t)min(first + j * STEP, S - 1) * rows + at) * DH + c0);
+  const int h = (int)(at % a.H), tok = (int)(at / a.H % a.r.max_rows);
+  const int s = (int)(at / a.H / a.r.max_rows);
+  const SeqRows sr = seq_rows(a.r, s);
+  if (tok >= sr.n) return;
   const float m = wave_max(st.x);
   const bool used = !(st.x == -INFINITY && st.y == 0.f);
   const float w = used ? __builtin_amdgcn_exp2f(st.x - m) : 0.f;
   const float l = wave_sum(used ? w * st.y : 0.f);
-  const int c0 = (lane & (LR - 1)) * 4, first = (W == 1 ? 0 : wave * P) + lane / LR;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int k0 = 0; k0 < S; k0 += (W == 1 ? 1 : 4) * P) {
-    const int k = k0 + first;
-    const float4 p = *reinterpret_cast<const float4*>(a.work + ((int64_t)min(k, S - 1) * rows + at) * DH + c0);
-    const float wk = k < S ? __shfl(w, k) : 0.f;
-    if (wk != 0.f) {  // (a split that saw nothing may hold anything)
-      o.x += wk * p.x; o.y += wk * p.y; o.z += wk * p.z; o.w += wk * p.w;
+  for (int k0 = 0; k0 < S; k0 += STEP * AHEAD) {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int k = k0 + j * STEP + first;
+      const float wk = __shfl(w, min(k, S - 1));
+      if (k < S && wk != 0.f) {  // (a split that saw nothing may hold anything)
+        o.x += wk * p[j].x; o.y += wk * p[j].y; o.z += wk * p[j].z; o.w += wk * p[j].w;
+      }
+      if (k0 + STEP * AHEAD < S) p[j] = *reinterpret_cast<const float4*>(a.work + ((int64_t)min(k + STEP * AHEAD, S - 1) * rows + at) * DH + c0);
     }
   }
   o.x = across_sum<LR>(o.x); o.y = across_sum<LR>(o.y); o.z = across_sum<LR>(o.z); o.w = across_sum<LR>(o.w);
@@ -1085,9 +1177,11 @@ struct Plan {
 
 // Waves of a wide step block: what the registers of a compute unit hold of it.
 constexpr int wide_waves(int type, int dh) { return dh == 128 || type == PT_MXFP4 ? 8 : 16; }
-#ifndef KWIDE
-#define KWIDE 4096
-#endif
+// Slots that a wide block takes in one round of its waves: up to these it needs no split and
+// no join (us in a graph, B = 1, wide and split: float16 d = 64, 512 slots 7.5 and 7.8, 1024
+// 9.9 and 7.9; bfloat16 d = 128, 512 8.9 and 9.1; MXFP4 d = 64, 512 6.1 and 7.6, 1024 7.8 and
+// 7.7; d = 128, 512 6.8 and 8.2, 1024 9.1 and 8.7).
+constexpr int wide_slots(int type) { return type == PT_MXFP4 ? 1024 : 512; }
 
 Plan plan_of(const PagedCache& c, const PagedRows& r, int H) {
   Plan p;
@@ -1101,7 +1195,7 @@ Plan plan_of(const PagedCache& c, const PagedRows& r, int H) {
   const int64_t want = (p.step ? kStepBlocks : kPromptBlocks) / std::max<int64_t>(blocks, 1);
   int64_t S = std::min<int64_t>(std::min<int64_t>(want, kMaxSplits), (slots + 255) / 256);
   S = std::max<int64_t>(S, 1);
-  p.wide = p.step && S > 1 && slots * c.dh <= KWIDE * 64;
+  p.wide = p.step && S > 1 && slots <= wide_slots(c.type);
   if (p.wide) S = 1;
   p.g.chunk = (int)(((slots + S - 1) / S + 63) / 64 * 64);
   p.g.S = (int)((slots + p.g.chunk - 1) / p.g.chunk);
@@ -1150,7 +1244,7 @@ hipError_t attend_ct(const PagedAttend& a, const Plan& p, hipStream_t st, const 
 
 size_t paged_work_bytes(const PagedCache& c, const PagedRows& r, int H) {
   const Plan p = plan_of(c, r, H);
-  return p.g.S > 1 ? (size_t)p.g.S * r.n_rows * H * (c.dh + 2) * 4 : 0;
+  return p.g.S > 1 ? (size_t)p.g.S * c.n_seqs * r.max_rows * H * (c.dh + 2) * 4 : 0;
 }
 
 // A split launch has at most so many blocks, of 16 or 128 packed rows each.
@@ -1158,23 +1252,55 @@ size_t paged_work_most(int dh) {
   return (size_t)std::max(16 * kStepBlocks, 128 * kPromptBlocks) * (dh + 2) * 4;
 }
 
+// Rows of a wave: 16 (four times four in flight) where that leaves 8192 waves, 32 for each
+// compute unit, else 4 or 1.
+static Tasks tasks_of(int heads0, int heads, int dh, int n_rows, uint32_t* blocks) {
+  Tasks t;
+  t.per_shift = dh == 32 ? 2 : dh == 64 ? 3 : 4;
+  const int c0 = ((heads0 << t.per_shift) + 63) / 64, c1 = ((heads << t.per_shift) + 63) / 64;
+  t.first[0] = 0;
+  t.first[1] = c0;
+  t.first[2] = c0 + c1;
+  t.chunks = c0 + 2 * c1;
+  const int64_t waves = (int64_t)n_rows * t.chunks;
+  t.rows = waves >= 16 * 8192 ? 16 : waves >= 4 * 8192 ? 4 : 1;
+  *blocks = (uint32_t)(((int64_t)(n_rows + t.rows - 1) / t.rows * t.chunks + 3) / 4);
+  return t;
+}
+
+template <int CT>
+static hipError_t append_ct(const PagedAppend& a, hipStream_t st, const Ev& ev) {
+  uint32_t blocks;
+  const Tasks t = tasks_of(a.q.p != nullptr ? a.H : 0, a.c.hk, a.c.dh, a.r.n_rows, &blocks);
+  if (t.rows == 1) return plaunch(paged_append_kernel<CT, 1>, dim3(blocks), dim3(256), st, ev.start, ev.stop, a, t);
+  return plaunch(paged_append_kernel<CT, 4>, dim3(blocks), dim3(256), st, ev.start, ev.stop, a, t);
+}
+
+template <int CT>
+static hipError_t read_ct(const PagedCache& c, const PagedRows& r, const HeadRows& k, const HeadRows& v, hipStream_t st, const Ev& ev) {
+  uint32_t blocks;
+  const Tasks t = tasks_of(0, c.hk, c.dh, r.n_rows, &blocks);
+  if (t.rows == 1) return plaunch(paged_read_kernel<CT, 1>, dim3(blocks), dim3(256), st, ev.start, ev.stop, c, r, k, v, t);
+  return plaunch(paged_read_kernel<CT, 4>, dim3(blocks), dim3(256), st, ev.start, ev.stop, c, r, k, v, t);
+}
+
 hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st, const Ev& ev) {
-  const int units = ((a.q.p != nullptr ? a.H : 0) + 2 * a.c.hk) * (a.c.dh / 8);
-  const int64_t all = (int64_t)units * a.r.n_rows;
-  const dim3 grid((uint32_t)((all + 255) / 256));
   switch (a.c.type) {
-    case PT_BF16: return plaunch(paged_append_kernel<PT_BF16>, grid, dim3(256), st, ev.start, ev.stop, a, units, all);
-    case PT_F16: return plaunch(paged_append_kernel<PT_F16>, grid, dim3(256), st, ev.start, ev.stop, a, units, all);
-    case PT_MXFP4: return plaunch(paged_append_kernel<PT_MXFP4>, grid, dim3(256), st, ev.start, ev.stop, a, units, all);
+    case PT_BF16: return append_ct<PT_BF16>(a, st, ev);
+    case PT_F16: return append_ct<PT_F16>(a, st, ev);
+    case PT_MXFP4: return append_ct<PT_MXFP4>(a, st, ev);
     default: return hipErrorInvalidValue;
   }
 }
 
 hipError_t launch_paged_read(const PagedCache& c, const PagedRows& r, const HeadRows& k, const HeadRows& v, hipStream_t st,
                              const Ev& ev) {
-  const int units = 2 * c.hk * (c.dh / 8);
-  const int64_t all = (int64_t)units * r.n_rows;
-  return plaunch(paged_read_kernel, dim3((uint32_t)((all + 255) / 256)), dim3(256), st, ev.start, ev.stop, c, r, k, v, units, all);
+  switch (c.type) {
+    case PT_BF16: return read_ct<PT_BF16>(c, r, k, v, st, ev);
+    case PT_F16: return read_ct<PT_F16>(c, r, k, v, st, ev);
+    case PT_MXFP4: return read_ct<PT_MXFP4>(c, r, k, v, st, ev);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 hipError_t launch_paged_attend(const PagedAttend& a, hipStream_t st, const Ev& ev) {
