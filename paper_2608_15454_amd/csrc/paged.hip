@@ -255,14 +255,16 @@ __device__ __forceinline__ float round_odd(double d) {
 }
 
 // ------------------------------------------------------------------- append ----
-// Every value is read once and written once, so the copy rate bounds it; the rotation is
-// three operations a channel.  U rows' loads are in flight together.
-template <int CT, int U>
+// Every value is read once and written once, so the copy rate bounds it (4.7 TB/s for a
+// large copy): 4.6 to 5.4 TB/s with float32 rows, 4.1 from 16-bit rows into MXFP4.  The
+// rotation is three operations a channel.  One row at a time: with two or four rows' loads
+// in flight the code of the rows' cases, that many times unrolled, was slower (8 prompts
+// of 32 + 2 x 8 heads of 128 bfloat16 channels into MXFP4: 127, 141 and 175 us).
+template <int CT>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, Tasks tk) {
   const Lane l = lane_of(tk, a.H, a.c.hk);
   const int dh = a.c.dh;
   if (l.row0 >= a.r.n_rows) return;
-  RowSeq f = seq_of(a.r, a.c.n_seqs, l.row0);
   const HeadRows src = l.which == 0 ? a.q : l.which == 1 ? a.k : a.v;
   const bool turn = l.which < 2 && a.rope != nullptr;
   const int64_t at_src = (int64_t)l.h * src.head + l.c0, at_out = (int64_t)l.h * a.qo.head + l.c0;
@@ -270,39 +272,41 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, Tasks 
   char* const pool = l.which == 1 ? a.c.k : a.c.v;
   const int es = src.type == PT_F32 ? 4 : 2;
   const int last = min(l.row0 + tk.rows, a.r.n_rows);
-  Raw8 raw[U];
-  float4 cs[U][2];
-  int32_t slot[U], id[U];
-  bool ok[U];
-  auto fetch = [&](int row, int j) {
-    advance(a.r, a.c.n_seqs, row, &f);
-    slot[j] = slot_of(f, row);
-    ok[j] = row < last && f.s >= 0 && row >= f.start && row < f.end;
-    int32_t pos = slot[j];
-    if (a.rope != nullptr) {
-      if (a.pos != nullptr) pos = a.pos[min(row, a.r.n_rows - 1)];
-      ok[j] = ok[j] && (uint32_t)pos < (uint32_t)a.n_pos;
-    }
-    id[j] = -1;
-    if (l.which > 0 && slot[j] >= 0 && (slot[j] >> a.c.shift) < a.c.max_pages)
-      id[j] = a.c.pages[(int64_t)f.s * a.c.max_pages + (slot[j] >> a.c.shift)];
-    if (!ok[j]) return;
-    if (l.live) {
-      load_raw8(reinterpret_cast<const char*>(src.p) + (int64_t)row * src.row * es, at_src, src.type, src.vec, raw[j]);
-      if (turn) {
-        const float4* t = reinterpret_cast<const float4*>(a.rope + (int64_t)pos * (dh / 2)) + l.c0 / 4;
-        cs[j][0] = t[0];
-        cs[j][1] = t[1];
-      }
-    }
+  // a row's values are loaded before its place is known, the next row's during this one
+  Raw8 ahead;
+  auto fetch = [&](int row) {
+    if (l.live) load_raw8(reinterpret_cast<const char*>(src.p) + (int64_t)row * src.row * es, at_src, src.type, src.vec, ahead);
   };
-  auto put = [&](int row, int j) {
+  fetch(l.row0);
+  RowSeq f = seq_of(a.r, a.c.n_seqs, l.row0);
+  for (int row = l.row0; row < last; ++row) {
+    const Raw8 raw = ahead;
+    if (row + 1 < last) fetch(row + 1);
+    advance(a.r, a.c.n_seqs, row, &f);
+    if (f.s < 0 || row < f.start || row >= f.end) continue;
+    const int32_t slot = slot_of(f, row);
+    int32_t pos = slot, id = -1;
+    if (a.rope != nullptr) {
+      if (a.pos != nullptr) pos = a.pos[row];
+      if ((uint32_t)pos >= (uint32_t)a.n_pos) continue;
+    }
+    if (l.which > 0) {
+      if (slot >= 0 && (slot >> a.c.shift) < a.c.max_pages) id = a.c.pages[(int64_t)f.s * a.c.max_pages + (slot >> a.c.shift)];
+      if ((uint32_t)id >= (uint32_t)a.c.n_pages) continue;
+    }
+    if (!l.live) continue;
+    float4 cs[2];
+    if (turn) {
+      const float4* t = reinterpret_cast<const float4*>(a.rope + (int64_t)pos * (dh / 2)) + l.c0 / 4;
+      cs[0] = t[0];
+      cs[1] = t[1];
+    }
     float x[8];
-    values8(raw[j], src.type, x);
+    values8(raw, src.type, x);
     if ((l.which == 0 || CT != PT_MXFP4) && turn) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float c = i & 1 ? cs[j][i >> 1].z : cs[j][i >> 1].x, sn = i & 1 ? cs[j][i >> 1].w : cs[j][i >> 1].y;
+        const float c = i & 1 ? cs[i >> 1].z : cs[i >> 1].x, sn = i & 1 ? cs[i >> 1].w : cs[i >> 1].y;
         const float r0 = x[2 * i] * c - x[2 * i + 1] * sn, r1 = x[2 * i] * sn + x[2 * i + 1] * c;
         x[2 * i] = r0;
         x[2 * i + 1] = r1;
@@ -310,11 +314,10 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, Tasks 
     }
     if (l.which == 0) {
       store_n(reinterpret_cast<char*>(a.qo.p) + (int64_t)row * a.qo.row * es, at_out, a.qo.type, a.qo.vec, x);
-      return;
+      continue;
     }
-    if ((uint32_t)id[j] >= (uint32_t)a.c.n_pages) return;
-    char* page = pool + (int64_t)id[j] * a.c.hk * a.c.page_bytes + head;
-    const int at = slot[j] & ((1 << a.c.shift) - 1);
+    char* page = pool + (int64_t)id * a.c.hk * a.c.page_bytes + head;
+    const int at = slot & ((1 << a.c.shift) - 1);
     if constexpr (CT != PT_MXFP4) {
       if constexpr (CT == PT_F16) {  // finite values beyond the type's largest are held as that
 #pragma unroll
@@ -332,7 +335,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, Tasks 
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const double c = i & 1 ? cs[j][i >> 1].z : cs[j][i >> 1].x, sn = i & 1 ? cs[j][i >> 1].w : cs[j][i >> 1].y;
+          const double c = i & 1 ? cs[i >> 1].z : cs[i >> 1].x, sn = i & 1 ? cs[i >> 1].w : cs[i >> 1].y;
           d[2 * i] = (double)x[2 * i] * c - (double)x[2 * i + 1] * sn;
           d[2 * i + 1] = (double)x[2 * i] * sn + (double)x[2 * i + 1] * c;
         }
@@ -353,13 +356,6 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, Tasks 
       *reinterpret_cast<uint32_t*>(page + (at * dh + l.c0) / 2) = u;
       if ((l.c0 & 31) == 0) page[(dh / 2 << a.c.shift) + at * (dh >> 5) + (l.c0 >> 5)] = (char)byte;
     }
-  };
-  for (int row = l.row0; row < last; row += U) {
-#pragma unroll
-    for (int j = 0; j < U; ++j) fetch(row + j, j);
-#pragma unroll
-    for (int j = 0; j < U; ++j)
-      if (ok[j] && l.live) put(row + j, j);
   }
 }
 
@@ -1018,15 +1014,18 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
       const uint16_t* vt = lds[cur][1];
       f32x16 sc[2];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[b][r] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + (32 * b + col) * PITCH + ks * 16 + half * 8);
+      for (int ks = 0; ks < KS; ++ks) {
+        u32x4 kf[2];
 #pragma unroll
-          for (int n = 0; n < T::kQ; ++n) sc[b] = mma32<CT>(kf, q[ks][n], sc[b]);
-        }
+        for (int b = 0; b < 2; ++b) kf[b] = *reinterpret_cast<const u32x4*>(kt + (32 * b + col) * PITCH + ks * 16 + half * 8);
+#pragma unroll
+        for (int n = 0; n < T::kQ; ++n)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) sc[b] = mma32<CT>(kf[b], q[ks][n], sc[b]);
       }
       uint32_t ok = 0;
 #pragma unroll
@@ -1035,6 +1034,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
         ok |= (uint32_t)((uint32_t)id < (uint32_t)a.c.n_pages) << b;
       }
       if (t < lo_all || t + KT > hi_all || ok != 15u) {
+        asm volatile("" ::: "memory");  // a branch, not selects in every tile
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -1049,20 +1049,22 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[b][r]);
       mx = pair_max<32>(mx);
-      const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn * f;
-      const float alpha = __builtin_amdgcn_exp2f(m * f - ref);
-      m = mn;
-      float ls = 0.f;
+      if (__any(mx * f > fmaf(m, f, kSlack) || m == -INFINITY)) {
+        const float mn = fmaxf(m, mx);
+        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * f);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) o[cb] *= alpha;
+      }
+      const float ref = m == -INFINITY ? 0.f : m * f;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           sc[b][r] = __builtin_amdgcn_exp2f(fmaf(sc[b][r], f, -ref));
-          ls += sc[b][r];
+          l += sc[b][r];
         }
-      l = l * alpha + ls;
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) o[cb] *= alpha;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -1073,13 +1075,16 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
           split8<CT, T::kP>(x, p);
           // lanes of a quarter wave: channels 16 (lane / 16 % 2) .., slots 4 half .. of the 8
           const uint16_t* src = vt + (32 * b + 16 * k2 + 4 * half + ((lane & 15) >> 2)) * PITCH + (lane & 16) + (lane & 3) * 4;
+          u32x4 vf[CB];
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb) {
             const uint2 v0 = read_turned(src + cb * 32), v1 = read_turned(src + 8 * PITCH + cb * 32);
-            const u32x4 vf = {v0.x, v0.y, v1.x, v1.y};
-#pragma unroll
-            for (int n = 0; n < T::kP; ++n) o[cb] = mma32<CT>(vf, p[n], o[cb]);
+            vf[cb] = u32x4{v0.x, v0.y, v1.x, v1.y};
           }
+#pragma unroll
+          for (int n = 0; n < T::kP; ++n)
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) o[cb] = mma32<CT>(vf[cb], p[n], o[cb]);
         }
     }
     if (more) store(cur ^ 1);
@@ -1252,8 +1257,7 @@ size_t paged_work_most(int dh) {
   return (size_t)std::max(16 * kStepBlocks, 128 * kPromptBlocks) * (dh + 2) * 4;
 }
 
-// Rows of a wave: 16 (four times four in flight) where that leaves 8192 waves, 32 for each
-// compute unit, else 4 or 1.
+// Rows of a wave: 4 where that leaves 8192 waves, 32 for each compute unit.
 static Tasks tasks_of(int heads0, int heads, int dh, int n_rows, uint32_t* blocks) {
   Tasks t;
   t.per_shift = dh == 32 ? 2 : dh == 64 ? 3 : 4;
@@ -1263,7 +1267,7 @@ static Tasks tasks_of(int heads0, int heads, int dh, int n_rows, uint32_t* block
   t.first[2] = c0 + c1;
   t.chunks = c0 + 2 * c1;
   const int64_t waves = (int64_t)n_rows * t.chunks;
-  t.rows = waves >= 16 * 8192 ? 16 : waves >= 4 * 8192 ? 4 : 1;
+  t.rows = waves >= 4 * 8192 ? 4 : 1;
   *blocks = (uint32_t)(((int64_t)(n_rows + t.rows - 1) / t.rows * t.chunks + 3) / 4);
   return t;
 }
@@ -1272,8 +1276,7 @@ template <int CT>
 static hipError_t append_ct(const PagedAppend& a, hipStream_t st, const Ev& ev) {
   uint32_t blocks;
   const Tasks t = tasks_of(a.q.p != nullptr ? a.H : 0, a.c.hk, a.c.dh, a.r.n_rows, &blocks);
-  if (t.rows == 1) return plaunch(paged_append_kernel<CT, 1>, dim3(blocks), dim3(256), st, ev.start, ev.stop, a, t);
-  return plaunch(paged_append_kernel<CT, 4>, dim3(blocks), dim3(256), st, ev.start, ev.stop, a, t);
+  return plaunch(paged_append_kernel<CT>, dim3(blocks), dim3(256), st, ev.start, ev.stop, a, t);
 }
 
 template <int CT>
@@ -1281,7 +1284,7 @@ static hipError_t read_ct(const PagedCache& c, const PagedRows& r, const HeadRow
   uint32_t blocks;
   const Tasks t = tasks_of(0, c.hk, c.dh, r.n_rows, &blocks);
   if (t.rows == 1) return plaunch(paged_read_kernel<CT, 1>, dim3(blocks), dim3(256), st, ev.start, ev.stop, c, r, k, v, t);
-  return plaunch(paged_read_kernel<CT, 4>, dim3(blocks), dim3(256), st, ev.start, ev.stop, c, r, k, v, t);
+  return plaunch(paged_read_kernel<CT, 2>, dim3(blocks), dim3(256), st, ev.start, ev.stop, c, r, k, v, t);
 }
 
 hipError_t launch_paged_append(const PagedAppend& a, hipStream_t st, const Ev& ev) {
