@@ -606,7 +606,8 @@ __global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_ke
   using T = Terms<CT, QT>;
   constexpr bool F4 = CT == PT_MXFP4;
   constexpr int KT = DH == 128 ? 32 : F4 || DH == 32 ? 64 : 32;
-  constexpr int NB = KT / 16, KS = DH / 32, CB = DH / 16, PITCH = DH + 8;
+  constexpr int NB = KT / 16, KS = DH / 32, CB = DH / 16;
+  constexpr int PITCH = DH + 16;  // half a wave reads 32 bytes of 8 slots turned round: 8 x 32 bytes in different banks
   constexpr int VU = F4 ? KT * DH / 32 / 64 : KT * DH / 8 / 64;  // 16-byte pieces of a block's values per lane
   static_assert(VU >= 1, "a block has a piece for every lane");
   constexpr int TILE = KT * PITCH * 2, MERGE = 16 * (DH + 4) * 4;
@@ -618,11 +619,10 @@ __global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_ke
   const int32_t* const ids = a.c.pages + (int64_t)s * a.c.max_pages;
   // The ids of a block's pages are fetched one block before its keys, so that no load waits
   // for the load of its address.
-  int32_t ahead[NB];
-  auto fetch_ids = [&](int t) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b) ahead[b] = ids[min((t + 16 * b) >> a.c.shift, a.c.max_pages - 1)];
-  };
+  // (a vector load, lane i the page of the block's 16-slot part i: scalar loads return out
+  // of order, so that every wait for LDS would wait for them too.)
+  int32_t ahead;
+  auto fetch_ids = [&](int t) { ahead = ids[min((t + 16 * (lane & (NB - 1))) >> a.c.shift, a.c.max_pages - 1)]; };
   // without lower ends the split's first slots are known at once, and their pages' ids are
   // loaded beside the sequence's rows
   fetch_ids(a.lo == nullptr ? (int)min((int64_t)split * gr.chunk, (int64_t)cap) + wave * KT : 0);
@@ -663,8 +663,9 @@ __global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_ke
     int64_t pg[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const bool ok = t + 16 * b < kmax && (uint32_t)ahead[b] < (uint32_t)a.c.n_pages;
-      pg[b] = ((int64_t)(ok ? ahead[b] : 0) * a.c.hk + kvh) * a.c.page_bytes;
+      const int32_t id = __builtin_amdgcn_readlane(ahead, b);
+      const bool ok = t + 16 * b < kmax && (uint32_t)id < (uint32_t)a.c.n_pages;
+      pg[b] = ((int64_t)(ok ? id : 0) * a.c.hk + kvh) * a.c.page_bytes;
       valid |= (uint32_t)ok << b;
     }
     fetch_ids(t + step);
@@ -885,13 +886,29 @@ template <int CT, int DH, int QT>
 __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Grid gr) {
   using T = Terms<CT, QT, DH == 128 ? 2 : 3>;
   constexpr bool F4 = CT == PT_MXFP4;
-  constexpr int KT = 64, KS = DH / 16, CB = DH / 32, PITCH = DH + 8;
+  // 64 slots a tile, 32 where two terms of 128 channels fill the registers
+  constexpr int KT = DH == 128 && T::kQ > 1 ? 32 : 64, NB = KT / 32, NG = KT / 16, KS = DH / 16, CB = DH / 32;
+  // distances of two slots in LDS: keys are read 16 bytes of 8 slots at a time; of values,
+  // half a wave reads 64 bytes of 4 slots turned round: 64 bytes off a multiple of 256, they
+  // lie in different banks
+  constexpr int PITCH = DH + 8, VP = DH == 128 ? 160 : DH == 64 ? 96 : 32;
   // pieces of a tile: 16 bytes (16-bit types: 8 channels, codes: 16 channels of 8 bytes)
   constexpr int PER = F4 ? DH / 16 : DH / 8, PIECES = KT * PER, NP = PIECES < 256 ? 1 : PIECES / 256;
-  __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][KT * PITCH];
+  __shared__ __attribute__((aligned(16))) uint16_t lds_k[2][KT * PITCH], lds_v[2][KT * VP];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
+  // Blocks go to the 8 XCDs in turn.  With a multiple of 8 (sequence, KV head) pairs, a
+  // pair's blocks all go to one, whose L2 then holds its keys and values (from four pairs
+  // for each XCD on: with fewer, ragged sequences leave some XCDs without work).
+  int bx = blockIdx.x, kvh = blockIdx.y, s = blockIdx.z;
+  if (((gridDim.y * gridDim.z) & 7) == 0 && gridDim.y * gridDim.z >= 32) {
+    const uint32_t id = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), at = id >> 3, round = at / gridDim.x;
+    const uint32_t pair = round * 8 + (id & 7);
+    bx = (int)(at - round * gridDim.x);
+    s = (int)(pair / gridDim.y);
+    kvh = (int)(pair - s * gridDim.y);
+  }
   // late rows see the most slots: they go first
-  const int at_x = blockIdx.x / gr.S, tile = gr.tiles - 1 - at_x, split = blockIdx.x - at_x * gr.S, kvh = blockIdx.y, s = blockIdx.z;
+  const int at_x = bx / gr.S, tile = gr.tiles - 1 - at_x, split = bx - at_x * gr.S;
   const int G = gr.G;
   const SeqRows sr = seq_rows(a.r, s);
   const int nq = min(sr.n, a.r.max_rows) * G;
@@ -959,36 +976,64 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
   const int sc_off = DH / 2 << a.c.shift;
   u32x4 kr[NP], vr[NP];  // (codes: two words each)
   uint32_t ksc[NP], vsc[NP];
+  // ids of the pages of a tile's 16-slot parts, in the first lanes, loaded a tile before they
+  // are used
+  int32_t ahead;
+  auto fetch_ids = [&](int t) { ahead = ids[min((t + 16 * (lane & (NG - 1))) >> a.c.shift, a.c.max_pages - 1)]; };
+  uint32_t valid = 0;  // parts with a page, of the tile in the registers
   auto load = [&](int t) {
+    int64_t pg[NG];
+    valid = 0;
+#pragma unroll
+    for (int b = 0; b < NG; ++b) {
+      const int32_t id = __builtin_amdgcn_readlane(ahead, b);
+      const bool ok = (uint32_t)id < (uint32_t)a.c.n_pages;
+      pg[b] = ((int64_t)(ok ? id : 0) * a.c.hk + kvh) * a.c.page_bytes;
+      valid |= (uint32_t)ok << b;
+    }
 #pragma unroll
     for (int u = 0; u < NP; ++u) {
-      const int i = min(u * 256 + tid, PIECES - 1), key = i / PER, part = i % PER, n = (t + key) >> a.c.shift;
-      const int32_t id = ids[min(n, a.c.max_pages - 1)];
-      const bool ok = t + key >= kmin && t + key < kmax && (uint32_t)id < (uint32_t)a.c.n_pages;
-      const int64_t page = ((int64_t)(ok ? id : 0) * a.c.hk + kvh) * a.c.page_bytes;
-      const uint32_t at = (uint32_t)(t + key) & in_page;
+      // a wave's 64 pieces lie within one part (or in two, for 32 channels of codes)
+      const int i = min(u * 256 + tid, PIECES - 1), key = i / PER, piece = i % PER;
+      int64_t page = pg[min((u * 256 + wave * 64) / PER / 16, NG - 1)];
+      if constexpr (PER < 4) page = (key >> 4) & 1 ? pg[min((u * 256 + wave * 64) / PER / 16 + 1, NG - 1)] : page;
+      const uint32_t at = ((uint32_t)(t + (key & ~15)) & in_page) + (key & 15);
       if constexpr (F4) {
-        const uint2 x = *reinterpret_cast<const uint2*>(a.c.k + page + at * (DH / 2) + part * 8);
-        const uint2 y = *reinterpret_cast<const uint2*>(a.c.v + page + at * (DH / 2) + part * 8);
+        const uint2 x = *reinterpret_cast<const uint2*>(a.c.k + page + (at * (DH / 2) + piece * 8));
+        const uint2 y = *reinterpret_cast<const uint2*>(a.c.v + page + (at * (DH / 2) + piece * 8));
         kr[u][0] = x.x; kr[u][1] = x.y;
-        // codes of slots that no row may see: zeros
-        vr[u][0] = ok ? y.x : 0; vr[u][1] = ok ? y.y : 0;
-        ksc[u] = (uint8_t)a.c.k[page + sc_off + at * (DH / 32) + part / 2];
-        vsc[u] = ok ? (uint8_t)a.c.v[page + sc_off + at * (DH / 32) + part / 2] : 127;
+        vr[u][0] = y.x; vr[u][1] = y.y;
+        ksc[u] = (uint8_t)a.c.k[page + (sc_off + at * (DH / 32) + piece / 2)];
+        vsc[u] = (uint8_t)a.c.v[page + (sc_off + at * (DH / 32) + piece / 2)];
       } else {
-        kr[u] = *reinterpret_cast<const u32x4*>(a.c.k + page + at * (DH * 2) + part * 16);
-        const u32x4 y = *reinterpret_cast<const u32x4*>(a.c.v + page + at * (DH * 2) + part * 16);
-        vr[u] = ok ? y : u32x4{0, 0, 0, 0};
+        kr[u] = *reinterpret_cast<const u32x4*>(a.c.k + page + (at * (DH * 2) + piece * 16));
+        vr[u] = *reinterpret_cast<const u32x4*>(a.c.v + page + (at * (DH * 2) + piece * 16));
+      }
+    }
+    fetch_ids(t + KT);
+  };
+  // values of slots that no row of the block may see: zeros
+  auto clean = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+      const int key = min(u * 256 + tid, PIECES - 1) / PER;
+      if (!(t + key >= kmin && t + key < kmax && ((valid >> (key >> 4)) & 1))) {
+        vr[u] = u32x4{0, 0, 0, 0};
+        vsc[u] = 127;
       }
     }
   };
-  auto store = [&](int buf) {
+  auto store = [&](int t, int buf) {
+    if (t < kmin || t + KT > kmax || valid != (1u << NG) - 1) {
+      asm volatile("" ::: "memory");
+      clean(t);
+    }
 #pragma unroll
     for (int u = 0; u < NP; ++u) {
-      const int i = u * 256 + tid, key = i / PER, part = i % PER;
+      const int i = u * 256 + tid, key = i / PER, piece = i % PER;
       if (PIECES < 256 && i >= PIECES) continue;
-      uint16_t* kd = &lds[buf][0][key * PITCH + part * (DH / PER)];
-      uint16_t* vd = &lds[buf][1][key * PITCH + part * (DH / PER)];
+      uint16_t* kd = &lds_k[buf][key * PITCH + piece * (DH / PER)];
+      uint16_t* vd = &lds_v[buf][key * VP + piece * (DH / PER)];
       if constexpr (F4) {
         reinterpret_cast<u32x4*>(kd)[0] = decode8(kr[u][0], ksc[u]);
         reinterpret_cast<u32x4*>(kd)[1] = decode8(kr[u][1], ksc[u]);
@@ -1000,9 +1045,12 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
       }
     }
   };
+  uint32_t ok = 0;
   if (begin < end) {
+    fetch_ids(begin);
     load(begin);
-    store(0);
+    ok = valid;
+    store(begin, 0);
   }
   int cur = 0;
   for (int t = begin; t < end; t += KT, cur ^= 1) {
@@ -1010,33 +1058,27 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
     const bool more = t + KT < end;
     if (more) load(t + KT);
     if (t < wmax && t + KT > wmin) {
-      const uint16_t* kt = lds[cur][0];
-      const uint16_t* vt = lds[cur][1];
-      f32x16 sc[2];
+      const uint16_t* kt = lds_k[cur];
+      const uint16_t* vt = lds_v[cur];
+      f32x16 sc[NB];
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[b][r] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        u32x4 kf[2];
+        u32x4 kf[NB];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) kf[b] = *reinterpret_cast<const u32x4*>(kt + (32 * b + col) * PITCH + ks * 16 + half * 8);
+        for (int b = 0; b < NB; ++b) kf[b] = *reinterpret_cast<const u32x4*>(kt + (32 * b + col) * PITCH + ks * 16 + half * 8);
 #pragma unroll
         for (int n = 0; n < T::kQ; ++n)
 #pragma unroll
-          for (int b = 0; b < 2; ++b) sc[b] = mma32<CT>(kf[b], q[ks][n], sc[b]);
+          for (int b = 0; b < NB; ++b) sc[b] = mma32<CT>(kf[b], q[ks][n], sc[b]);
       }
-      uint32_t ok = 0;
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int32_t id = ids[min((t + 16 * b) >> a.c.shift, a.c.max_pages - 1)];
-        ok |= (uint32_t)((uint32_t)id < (uint32_t)a.c.n_pages) << b;
-      }
-      if (t < lo_all || t + KT > hi_all || ok != 15u) {
+      if (t < lo_all || t + KT > hi_all || ok != (1u << NG) - 1) {
         asm volatile("" ::: "memory");  // a branch, not selects in every tile
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int slot = t + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3);
@@ -1045,7 +1087,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
       }
       float mx = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[b][r]);
       mx = pair_max<32>(mx);
@@ -1059,14 +1101,14 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
       }
       const float ref = m == -INFINITY ? 0.f : m * f;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           sc[b][r] = __builtin_amdgcn_exp2f(fmaf(sc[b][r], f, -ref));
           l += sc[b][r];
         }
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int k2 = 0; k2 < 2; ++k2) {
           const float x[8] = {sc[b][8 * k2], sc[b][8 * k2 + 1], sc[b][8 * k2 + 2], sc[b][8 * k2 + 3],
@@ -1074,11 +1116,11 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
           u32x4 p[T::kP];
           split8<CT, T::kP>(x, p);
           // lanes of a quarter wave: channels 16 (lane / 16 % 2) .., slots 4 half .. of the 8
-          const uint16_t* src = vt + (32 * b + 16 * k2 + 4 * half + ((lane & 15) >> 2)) * PITCH + (lane & 16) + (lane & 3) * 4;
+          const uint16_t* src = vt + (32 * b + 16 * k2 + 4 * half + ((lane & 15) >> 2)) * VP + (lane & 16) + (lane & 3) * 4;
           u32x4 vf[CB];
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb) {
-            const uint2 v0 = read_turned(src + cb * 32), v1 = read_turned(src + 8 * PITCH + cb * 32);
+            const uint2 v0 = read_turned(src + cb * 32), v1 = read_turned(src + 8 * VP + cb * 32);
             vf[cb] = u32x4{v0.x, v0.y, v1.x, v1.y};
           }
 #pragma unroll
@@ -1087,7 +1129,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
             for (int cb = 0; cb < CB; ++cb) o[cb] = mma32<CT>(vf[cb], p[n], o[cb]);
         }
     }
-    if (more) store(cur ^ 1);
+    ok = valid;
+    if (more) store(t + KT, cur ^ 1);
   }
   l = pair_sum<32>(l);
   if (qi >= nq) return;
@@ -1173,7 +1216,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttend a, int S) {
 constexpr int kStepRows = 32;
 constexpr int kMaxSplits = 64;
 // blocks of a launch up to which the slots are split
-constexpr int kStepBlocks = 1024, kPromptBlocks = 512;
+constexpr int kStepBlocks = 1024, kPromptBlocks = 1024;
 
 struct Plan {
   bool step, wide;
@@ -1197,7 +1240,8 @@ Plan plan_of(const PagedCache& c, const PagedRows& r, int H) {
   p.g.tiles = (int)((packed + per - 1) / per);
   // enough blocks for the chip's 256 compute units, of at least 256 slots each
   const int64_t blocks = (int64_t)p.g.tiles * c.n_seqs * c.hk, slots = std::max(r.max_slots, 1);
-  const int64_t want = (p.step ? kStepBlocks : kPromptBlocks) / std::max<int64_t>(blocks, 1);
+  // (a prompt's blocks sit two to a compute unit: from 512 on all of them are busy)
+  const int64_t want = p.step ? kStepBlocks / std::max<int64_t>(blocks, 1) : blocks < 512 ? kPromptBlocks / std::max<int64_t>(blocks, 1) : 1;
   int64_t S = std::min<int64_t>(std::min<int64_t>(want, kMaxSplits), (slots + 255) / 256);
   S = std::max<int64_t>(S, 1);
   p.wide = p.step && S > 1 && slots <= wide_slots(c.type);
