@@ -601,8 +601,8 @@ constexpr int step_waves(int ct, int dh, int qt) {
 //   O^T += V^T P^T: the probabilities are already where the product wants them, values
 //     go through the wave's own LDS tile and are read turned round.
 // The next block's loads are in flight during a block's softmax and value product.
-template <int CT, int DH, int QT, int NW>
-__global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_kernel(PagedAttend a, Grid gr) {
+template <int CT, int DH, int QT>
+__global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel(PagedAttend a, Grid gr) {
   using T = Terms<CT, QT>;
   constexpr bool F4 = CT == PT_MXFP4;
   constexpr int KT = DH == 128 ? 32 : F4 || DH == 32 ? 64 : 32;
@@ -611,7 +611,7 @@ __global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_ke
   constexpr int VU = F4 ? KT * DH / 32 / 64 : KT * DH / 8 / 64;  // 16-byte pieces of a block's values per lane
   static_assert(VU >= 1, "a block has a piece for every lane");
   constexpr int TILE = KT * PITCH * 2, MERGE = 16 * (DH + 4) * 4;
-  __shared__ __attribute__((aligned(16))) char lds[NW * (TILE > MERGE ? TILE : MERGE)];
+  __shared__ __attribute__((aligned(16))) char lds[4 * (TILE > MERGE ? TILE : MERGE)];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int tile = gr.tiles == 1 ? 0 : blockIdx.x / gr.S, split = blockIdx.x - tile * gr.S, kvh = blockIdx.y, s = blockIdx.z;
   const int G = gr.G;
@@ -649,7 +649,7 @@ __global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_ke
   float m = -INFINITY, l = 0.f;
 
   uint16_t* const vt = reinterpret_cast<uint16_t*>(lds + wave * TILE);
-  constexpr int step = NW * KT;
+  constexpr int step = 4 * KT;
   u32x4 kr[NB][F4 ? 1 : KS], vr[VU];
   uint32_t ksc[NB], vsc[VU];
   const uint32_t in_page = (1u << a.c.shift) - 1;
@@ -849,14 +849,14 @@ __global__ __launch_bounds__(64 * NW, step_waves(CT, DH, QT)) void paged_step_ke
   // thread: query tid / 16, DH / 16 channels
   constexpr int N = DH / 16;
   const int qj = tid >> 4, c0 = (tid & 15) * N, q2 = tile * 16 + qj;
-  if (tid >= 256 || q2 >= nq) return;
+  if (q2 >= nq) return;
   float mj = -INFINITY, lj = 0.f, oj[N];
 #pragma unroll
-  for (int w = 0; w < NW; ++w) mj = fmaxf(mj, mb[(w * 16 + qj) * (DH + 4)]);
+  for (int w = 0; w < 4; ++w) mj = fmaxf(mj, mb[(w * 16 + qj) * (DH + 4)]);
 #pragma unroll
   for (int i = 0; i < N; ++i) oj[i] = 0.f;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
+  for (int w = 0; w < 4; ++w) {
     const float* p = mb + (w * 16 + qj) * (DH + 4);
     if (p[0] == -INFINITY && p[1] == 0.f) continue;  // saw nothing
     const float e = __builtin_amdgcn_exp2f(p[0] - mj);
@@ -1219,33 +1219,37 @@ constexpr int kMaxSplits = 64;
 constexpr int kStepBlocks = 1024, kPromptBlocks = 1024;
 
 struct Plan {
-  bool step, wide;
+  bool step;
   Grid g;
 };
 
-// Waves of a wide step block: what the registers of a compute unit hold of it.
-constexpr int wide_waves(int type, int dh) { return dh == 128 || type == PT_MXFP4 ? 8 : 16; }
-// Slots that a wide block takes in one round of its waves: up to these it needs no split and
-// no join (us in a graph, B = 1, wide and split: float16 d = 64, 512 slots 7.5 and 7.8, 1024
-// 9.9 and 7.9; bfloat16 d = 128, 512 8.9 and 9.1; MXFP4 d = 64, 512 6.1 and 7.6, 1024 7.8 and
-// 7.7; d = 128, 512 6.8 and 8.2, 1024 9.1 and 8.7).
-constexpr int wide_slots(int type) { return type == PT_MXFP4 ? 1024 : 512; }
+// Slots that a step block's waves take in one round.
+int round_of(const PagedCache& c) { return c.dh == 128 || (c.dh == 64 && c.type != PT_MXFP4) ? 128 : 256; }
 
+// A split costs a second launch (3 us) and its sums' way through memory, a block too few
+// leaves compute units idle.  Step blocks: none up to 512 slots (us in a graph, one sequence
+// of 16 heads of 64 float16 channels: 512 slots 6.4 alone, 7.5 split; 1024 9.3 and 7.3); behind them
+// splits of one round or more, at most 32 (16384 slots of 8 heads of 128: bfloat16 16.8 with
+// 32, 18.2 with 64; MXFP4 10.4 and 11.2) and 512 blocks (4 sequences of 2048 MXFP4 slots: 8.9
+// with 512, 11.0 with 1024); and twice that once a split still has 1024 slots, where the
+// stream of the cache is what counts.  Prompt blocks sit two to a compute unit: from 512 on
+// all are busy.
 Plan plan_of(const PagedCache& c, const PagedRows& r, int H) {
   Plan p;
   p.g.G = H / c.hk;
-  const int64_t packed = (int64_t)r.max_rows * (H / c.hk);
+  const int64_t packed = (int64_t)r.max_rows * p.g.G;
   p.step = packed <= kStepRows;
   const int64_t per = p.step ? 16 : 128;
   p.g.tiles = (int)((packed + per - 1) / per);
-  // enough blocks for the chip's 256 compute units, of at least 256 slots each
-  const int64_t blocks = (int64_t)p.g.tiles * c.n_seqs * c.hk, slots = std::max(r.max_slots, 1);
-  // (a prompt's blocks sit two to a compute unit: from 512 on all of them are busy)
-  const int64_t want = p.step ? kStepBlocks / std::max<int64_t>(blocks, 1) : blocks < 512 ? kPromptBlocks / std::max<int64_t>(blocks, 1) : 1;
-  int64_t S = std::min<int64_t>(std::min<int64_t>(want, kMaxSplits), (slots + 255) / 256);
-  S = std::max<int64_t>(S, 1);
-  p.wide = p.step && S > 1 && slots <= wide_slots(c.type);
-  if (p.wide) S = 1;
+  const int64_t blocks = std::max<int64_t>((int64_t)p.g.tiles * c.n_seqs * c.hk, 1), slots = std::max(r.max_slots, 1);
+  int64_t S = 1;
+  if (p.step) {
+    const int round = round_of(c);
+    if (slots > 512) S = std::max<int64_t>({1, std::min<int64_t>({kStepBlocks / 2 / blocks, (slots + round - 1) / round, 32}),
+                                            std::min<int64_t>({kStepBlocks / blocks, slots / 1024, kMaxSplits})});
+  } else if (blocks < 512) {
+    S = std::max<int64_t>(1, std::min<int64_t>({kPromptBlocks / blocks, slots / 256, kMaxSplits}));
+  }
   p.g.chunk = (int)(((slots + S - 1) / S + 63) / 64 * 64);
   p.g.S = (int)((slots + p.g.chunk - 1) / p.g.chunk);
   return p;
@@ -1253,12 +1257,10 @@ Plan plan_of(const PagedCache& c, const PagedRows& r, int H) {
 
 template <int CT, int DH, int QT>
 hipError_t attend_at(const PagedAttend& a, const Plan& p, hipStream_t st, const Ev& ev) {
-  constexpr int NW = wide_waves(CT, DH);
   const dim3 grid((uint32_t)(p.g.S * p.g.tiles), (uint32_t)a.c.hk, (uint32_t)a.c.n_seqs);
   const bool join = p.g.S > 1;
   hipError_t e;
-  if (p.wide) e = plaunch(paged_step_kernel<CT, DH, QT, NW>, grid, dim3(64 * NW), st, ev.start, join ? nullptr : ev.stop, a, p.g);
-  else if (p.step) e = plaunch(paged_step_kernel<CT, DH, QT, 4>, grid, dim3(256), st, ev.start, join ? nullptr : ev.stop, a, p.g);
+  if (p.step) e = plaunch(paged_step_kernel<CT, DH, QT>, grid, dim3(256), st, ev.start, join ? nullptr : ev.stop, a, p.g);
   else e = plaunch(paged_prompt_kernel<CT, DH, QT>, grid, dim3(256), st, ev.start, join ? nullptr : ev.stop, a, p.g);
   if (e != hipSuccess || !join) return e;
   const int64_t waves = (int64_t)a.c.n_seqs * a.r.max_rows * a.H;
