@@ -608,8 +608,10 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
   constexpr int KT = DH == 128 ? 32 : F4 || DH == 32 ? 64 : 32;
   constexpr int NB = KT / 16, KS = DH / 32, CB = DH / 16;
   constexpr int PITCH = DH + 16;  // half a wave reads 32 bytes of 8 slots turned round: 8 x 32 bytes in different banks
-  constexpr int VU = F4 ? KT * DH / 32 / 64 : KT * DH / 8 / 64;  // 16-byte pieces of a block's values per lane
-  static_assert(VU >= 1, "a block has a piece for every lane");
+  // values are loaded 16 slots or fewer at a time, so that a load's page is the same in all
+  // lanes: VB bytes a lane, PER lanes a slot, VU loads a block
+  constexpr int ROW = F4 ? DH / 2 : DH * 2, VB = ROW >= 64 ? 16 : ROW / 4, PER = ROW / VB, ROWS = 64 / PER, VU = KT / ROWS;
+  static_assert(ROWS <= 16 && VB >= 4, "pieces");
   constexpr int TILE = KT * PITCH * 2, MERGE = 16 * (DH + 4) * 4;
   __shared__ __attribute__((aligned(16))) char lds[4 * (TILE > MERGE ? TILE : MERGE)];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
@@ -653,57 +655,60 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
   u32x4 kr[NB][F4 ? 1 : KS], vr[VU];
   uint32_t ksc[NB], vsc[VU];
   const uint32_t in_page = (1u << a.c.shift) - 1;
-  const int sc_off = DH / 2 << a.c.shift;
+  const uint32_t sc_off = DH / 2 << a.c.shift;
+  // bytes of a page of all heads, and where this head's begin: both below 2^32
+  const uint32_t stride = (uint32_t)(a.c.hk * a.c.page_bytes), head_at = (uint32_t)(kvh * a.c.page_bytes);
+  const uint32_t k_off = col * ROW + g * (ROW / 4), ks_off = col * (DH / 32) + g * DH / 128;
+  const uint32_t v_key = lane / PER, v_off = v_key * ROW + (lane % PER) * VB, vs_off = v_key * (DH / 32) + (lane % PER) * VB / 16;
   uint32_t valid = 0;  // of the block whose keys are in the registers: a bit for each 16 slots
   // Loads of the block at slot t.  16 slots never cross a page; slots at and behind kmax
   // are read from their page where there is one (any content is masked) and from page 0
   // where not.
   auto load = [&](int t) {
-    valid = 0;
-    int64_t pg[NB];
+    uint64_t pg[NB];
+    // parts behind kmax or without a page: page 0, and masked
+    const bool there = t + 16 * lane < kmax && (uint32_t)ahead < (uint32_t)a.c.n_pages;
+    valid = (uint32_t)__ballot(there) & ((1u << NB) - 1);
+    const int32_t id = there ? ahead : 0;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int32_t id = __builtin_amdgcn_readlane(ahead, b);
-      const bool ok = t + 16 * b < kmax && (uint32_t)id < (uint32_t)a.c.n_pages;
-      pg[b] = ((int64_t)(ok ? id : 0) * a.c.hk + kvh) * a.c.page_bytes;
-      valid |= (uint32_t)ok << b;
-    }
+    for (int b = 0; b < NB; ++b) pg[b] = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(id, b) * stride + head_at;
     fetch_ids(t + step);
+    // a scalar base and a lane's own offset, which stays from block to block
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const char* kp = a.c.k + pg[b];
-      const uint32_t at = ((uint32_t)(t + 16 * b) & in_page) + col;
+      const uint32_t at = (uint32_t)(t + 16 * b) & in_page;
+      const char* kp = a.c.k + (pg[b] + at * ROW);
       if constexpr (F4) {
-        const char* p = kp + at * (DH / 2) + g * (DH / 8);
         if constexpr (DH == 128) {
-          kr[b][0] = *reinterpret_cast<const u32x4*>(p);
+          kr[b][0] = *reinterpret_cast<const u32x4*>(kp + k_off);
         } else if constexpr (DH == 64) {
-          const uint2 u = *reinterpret_cast<const uint2*>(p);
+          const uint2 u = *reinterpret_cast<const uint2*>(kp + k_off);
           kr[b][0][0] = u.x;
           kr[b][0][1] = u.y;
         } else {
-          kr[b][0][0] = *reinterpret_cast<const uint32_t*>(p);
+          kr[b][0][0] = *reinterpret_cast<const uint32_t*>(kp + k_off);
         }
-        ksc[b] = (uint8_t)kp[sc_off + at * (DH / 32) + g * DH / 128];
+        ksc[b] = *reinterpret_cast<const uint8_t*>(a.c.k + (pg[b] + sc_off + at * (DH / 32)) + ks_off);
       } else {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kr[b][ks] = *reinterpret_cast<const u32x4*>(kp + (at * DH + g * (DH / 4) + ks * 8) * 2);
+        for (int ks = 0; ks < KS; ++ks) kr[b][ks] = *reinterpret_cast<const u32x4*>(kp + (k_off + ks * 16));
       }
     }
 #pragma unroll
     for (int u = 0; u < VU; ++u) {
-      // pieces of a block in slot order; the slots of piece u lie in the 16 slots b0
-      constexpr int PER = F4 ? DH / 32 : DH / 8, ROWS = 64 / PER;  // pieces of a slot, slots of one u
-      const int key = u * ROWS + lane / PER;
-      int64_t page = pg[(u * ROWS) / 16];
-      if constexpr (ROWS > 16) {
-#pragma unroll
-        for (int b = 1; b < ROWS / 16; ++b) page = key - u * ROWS >= 16 * b ? pg[(u * ROWS) / 16 + b] : page;
+      const uint32_t at = (uint32_t)(t + u * ROWS) & in_page;
+      const uint64_t page = pg[u * ROWS / 16];
+      const char* vp = a.c.v + (page + at * ROW);
+      if constexpr (VB == 16) {
+        vr[u] = *reinterpret_cast<const u32x4*>(vp + v_off);
+      } else if constexpr (VB == 8) {
+        const uint2 x = *reinterpret_cast<const uint2*>(vp + v_off);
+        vr[u][0] = x.x;
+        vr[u][1] = x.y;
+      } else {
+        vr[u][0] = *reinterpret_cast<const uint32_t*>(vp + v_off);
       }
-      const char* vp = a.c.v + page;
-      const uint32_t at = ((uint32_t)(t + (key & ~15)) & in_page) + (key & 15);
-      vr[u] = *reinterpret_cast<const u32x4*>(vp + at * (F4 ? DH / 2 : DH * 2) + (lane % PER) * 16);
-      if constexpr (F4) vsc[u] = (uint8_t)vp[sc_off + at * PER + lane % PER];
+      if constexpr (F4) vsc[u] = *reinterpret_cast<const uint8_t*>(a.c.v + (page + sc_off + at * (DH / 32)) + vs_off);
     }
   };
   int t = begin + wave * KT;
@@ -755,8 +760,7 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
       asm volatile("" ::: "memory");  // a branch, not selects in every block
 #pragma unroll
       for (int u = 0; u < VU; ++u) {
-        constexpr int PER = F4 ? DH / 32 : DH / 8, ROWS = 64 / PER;
-        const int key = u * ROWS + lane / PER;
+        const int key = u * ROWS + (int)v_key;
         if (!(t + key >= kmin && t + key < kmax && ((ok >> (key >> 4)) & 1))) {
           vr[u] = u32x4{0, 0, 0, 0};
           vsc[u] = 127;
@@ -765,14 +769,12 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
     }
 #pragma unroll
     for (int u = 0; u < VU; ++u) {
-      constexpr int PER = F4 ? DH / 32 : DH / 8, ROWS = 64 / PER;
-      const int key = u * ROWS + lane / PER;
+      uint16_t* d = vt + (u * ROWS + v_key) * PITCH + (lane % PER) * (DH / PER);
       if constexpr (F4) {
-        u32x4* d = reinterpret_cast<u32x4*>(vt + key * PITCH + (lane % PER) * 32);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] = decode8(vr[u][i], vsc[u]);
+        for (int i = 0; i < VB / 4; ++i) reinterpret_cast<u32x4*>(d)[i] = decode8(vr[u][i], vsc[u]);
       } else {
-        *reinterpret_cast<u32x4*>(vt + key * PITCH + (lane % PER) * 8) = vr[u];
+        *reinterpret_cast<u32x4*>(d) = vr[u];
       }
     }
     if (t + step < end) load(t + step);
@@ -973,7 +975,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
 
   const int32_t* const ids = a.c.pages + (int64_t)s * a.c.max_pages;
   const uint32_t in_page = (1u << a.c.shift) - 1;
-  const int sc_off = DH / 2 << a.c.shift;
+  const uint32_t sc_off = DH / 2 << a.c.shift;
+  const uint32_t stride = (uint32_t)(a.c.hk * a.c.page_bytes), head_at = (uint32_t)(kvh * a.c.page_bytes);
   u32x4 kr[NP], vr[NP];  // (codes: two words each)
   uint32_t ksc[NP], vsc[NP];
   // ids of the pages of a tile's 16-slot parts, in the first lanes, loaded a tile before they
@@ -982,20 +985,17 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
   auto fetch_ids = [&](int t) { ahead = ids[min((t + 16 * (lane & (NG - 1))) >> a.c.shift, a.c.max_pages - 1)]; };
   uint32_t valid = 0;  // parts with a page, of the tile in the registers
   auto load = [&](int t) {
-    int64_t pg[NG];
-    valid = 0;
+    uint64_t pg[NG];
+    const bool there = (uint32_t)ahead < (uint32_t)a.c.n_pages;
+    valid = (uint32_t)__ballot(there) & ((1u << NG) - 1);
+    const int32_t id = there ? ahead : 0;
 #pragma unroll
-    for (int b = 0; b < NG; ++b) {
-      const int32_t id = __builtin_amdgcn_readlane(ahead, b);
-      const bool ok = (uint32_t)id < (uint32_t)a.c.n_pages;
-      pg[b] = ((int64_t)(ok ? id : 0) * a.c.hk + kvh) * a.c.page_bytes;
-      valid |= (uint32_t)ok << b;
-    }
+    for (int b = 0; b < NG; ++b) pg[b] = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(id, b) * stride + head_at;
 #pragma unroll
     for (int u = 0; u < NP; ++u) {
       // a wave's 64 pieces lie within one part (or in two, for 32 channels of codes)
       const int i = min(u * 256 + tid, PIECES - 1), key = i / PER, piece = i % PER;
-      int64_t page = pg[min((u * 256 + wave * 64) / PER / 16, NG - 1)];
+      uint64_t page = pg[min((u * 256 + wave * 64) / PER / 16, NG - 1)];
       if constexpr (PER < 4) page = (key >> 4) & 1 ? pg[min((u * 256 + wave * 64) / PER / 16 + 1, NG - 1)] : page;
       const uint32_t at = ((uint32_t)(t + (key & ~15)) & in_page) + (key & 15);
       if constexpr (F4) {
