@@ -585,7 +585,7 @@ __device__ __forceinline__ void put_out(const PagedAttend& a, int S, int split, 
 
 // Waves per SIMD that a step kernel's registers leave room for without spills.
 constexpr int step_waves(int ct, int dh, int qt) {
-  if (dh < 128) return ct == PT_MXFP4 && dh == 64 && qt == PT_F32 ? 3 : 4;
+  if (dh < 128) return 4;
   return ct != PT_MXFP4 ? 2 : qt == PT_BF16 ? 4 : 3;
 }
 
@@ -605,7 +605,7 @@ template <int CT, int DH, int QT>
 __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel(PagedAttend a, Grid gr) {
   using T = Terms<CT, QT>;
   constexpr bool F4 = CT == PT_MXFP4;
-  constexpr int KT = DH == 128 ? 32 : F4 || DH == 32 ? 64 : 32;
+  constexpr int KT = DH == 32 ? 64 : 32;
   constexpr int NB = KT / 16, KS = DH / 32, CB = DH / 16;
   constexpr int PITCH = DH + 16;  // half a wave reads 32 bytes of 8 slots turned round: 8 x 32 bytes in different banks
   // values are loaded 16 slots or fewer at a time, so that a load's page is the same in all
@@ -916,7 +916,13 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
   const int nq = min(sr.n, a.r.max_rows) * G;
   if (tile * 128 >= nq) return;
   const int cap = a.c.max_pages << a.c.shift;
-  const int qi = tile * 128 + wave * 32 + col, tok = min(qi, nq - 1) / G, head = kvh * G + min(qi, nq - 1) - tok * G, row = sr.row0 + tok;
+  const int qi = tile * 128 + wave * 32 + col, tok = G == 1 ? min(qi, nq - 1) : min(qi, nq - 1) / G,
+            head = kvh * G + min(qi, nq - 1) - tok * G, row = sr.row0 + tok;
+  // the queries' loads go first; they are used once the first tile's are on their way
+  Raw8 raw[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+    load_raw8(a.q.p, (int64_t)row * a.q.row + (int64_t)head * a.q.head + ks * 16 + half * 8, QT, a.q.vec, raw[ks]);
   int lo = cap, hi = 0;
   if (qi < nq) row_range(a, sr, tok, cap, &lo, &hi);
   // the wave's extent: [wmin, wmax) holds every visible slot, all of [lo_all, hi_all) is
@@ -940,32 +946,6 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
   const int begin = __builtin_amdgcn_readfirstlane((int)min(b0, (int64_t)cap));
   const int end = __builtin_amdgcn_readfirstlane(split == gr.S - 1 ? kmax : (int)min((int64_t)kmax, b0 + gr.chunk));
 
-  float f = a.scale * 1.44269504f;
-  float sign = f < 0.f ? -1.f : f == 0.f ? 0.f : 1.f;
-  f = f == 0.f ? 1.f : fabsf(f);
-  u32x4 q[KS][T::kQ];
-  if constexpr (CT == PT_F16 && QT == PT_F32) {
-    float top = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      float x[8];
-      load8(a.q.p, (int64_t)row * a.q.row + (int64_t)head * a.q.head + ks * 16 + half * 8, QT, a.q.vec, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
-    }
-    top = pair_max<32>(top);
-    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
-    sign = ldexpf(sign, -e);
-    f = ldexpf(f, e);
-  }
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    float x[8];
-    load8(a.q.p, (int64_t)row * a.q.row + (int64_t)head * a.q.head + ks * 16 + half * 8, QT, a.q.vec, x);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] *= sign;
-    split8<CT, T::kQ>(x, q[ks]);
-  }
   f32x16 o[CB];
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb)
@@ -1046,9 +1026,35 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
     }
   };
   uint32_t ok = 0;
+  fetch_ids(begin);
+  if (begin < end) load(begin);
+  float f = a.scale * 1.44269504f;
+  float sign = f < 0.f ? -1.f : f == 0.f ? 0.f : 1.f;
+  f = f == 0.f ? 1.f : fabsf(f);
+  u32x4 q[KS][T::kQ];
+  if constexpr (CT == PT_F16 && QT == PT_F32) {
+    float top = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      float x[8];
+      values8(raw[ks], QT, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+    }
+    top = pair_max<32>(top);
+    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+    sign = ldexpf(sign, -e);
+    f = ldexpf(f, e);
+  }
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    float x[8];
+    values8(raw[ks], QT, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= sign;
+    split8<CT, T::kQ>(x, q[ks]);
+  }
   if (begin < end) {
-    fetch_ids(begin);
-    load(begin);
     ok = valid;
     store(begin, 0);
   }
@@ -1224,7 +1230,7 @@ struct Plan {
 };
 
 // Slots that a step block's waves take in one round.
-int round_of(const PagedCache& c) { return c.dh == 128 || (c.dh == 64 && c.type != PT_MXFP4) ? 128 : 256; }
+int round_of(const PagedCache& c) { return c.dh == 32 ? 256 : 128; }
 
 // A split costs a second launch (3 us) and its sums' way through memory, a block too few
 // leaves compute units idle.  Step blocks: none up to 512 slots (us in a graph, one sequence
