@@ -896,7 +896,13 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
   constexpr int PITCH = DH + 8, VP = DH == 128 ? 160 : DH == 64 ? 96 : 32;
   // pieces of a tile: 16 bytes (16-bit types: 8 channels, codes: 16 channels of 8 bytes)
   constexpr int PER = F4 ? DH / 16 : DH / 8, PIECES = KT * PER, NP = PIECES < 256 ? 1 : PIECES / 256;
-  __shared__ __attribute__((aligned(16))) uint16_t lds_k[2][KT * PITCH], lds_v[2][KT * VP];
+  // two tiles of keys and values; at the end each wave's outputs on their way to whole rows
+  constexpr int CP = DH < 64 ? DH : 64, OUT = 32 * (CP + 4);  // channels at a time, floats of a wave
+  constexpr int TILES = 2 * KT * (PITCH + VP) * 2;
+  static_assert(4 * OUT * 4 <= TILES, "the outputs fit the tiles' place");
+  __shared__ __attribute__((aligned(16))) char lds[TILES];
+  uint16_t* const lds_k = reinterpret_cast<uint16_t*>(lds);
+  uint16_t* const lds_v = lds_k + 2 * KT * PITCH;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
   // Blocks go to the 8 XCDs in turn.  With a multiple of 8 (sequence, KV head) pairs, a
   // pair's blocks all go to one, whose L2 then holds its keys and values (from four pairs
@@ -1012,8 +1018,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
     for (int u = 0; u < NP; ++u) {
       const int i = u * 256 + tid, key = i / PER, piece = i % PER;
       if (PIECES < 256 && i >= PIECES) continue;
-      uint16_t* kd = &lds_k[buf][key * PITCH + piece * (DH / PER)];
-      uint16_t* vd = &lds_v[buf][key * VP + piece * (DH / PER)];
+      uint16_t* kd = lds_k + (buf * KT + key) * PITCH + piece * (DH / PER);
+      uint16_t* vd = lds_v + (buf * KT + key) * VP + piece * (DH / PER);
       if constexpr (F4) {
         reinterpret_cast<u32x4*>(kd)[0] = decode8(kr[u][0], ksc[u]);
         reinterpret_cast<u32x4*>(kd)[1] = decode8(kr[u][1], ksc[u]);
@@ -1064,8 +1070,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
     const bool more = t + KT < end;
     if (more) load(t + KT);
     if (t < wmax && t + KT > wmin) {
-      const uint16_t* kt = lds_k[cur];
-      const uint16_t* vt = lds_v[cur];
+      const uint16_t* kt = lds_k + cur * KT * PITCH;
+      const uint16_t* vt = lds_v + cur * KT * VP;
       f32x16 sc[NB];
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -1139,7 +1145,6 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
     if (more) store(t + KT, cur ^ 1);
   }
   l = pair_sum<32>(l);
-  if (qi >= nq) return;
   if (hi == 0) {  // tiles that all other rows see whole were not masked for a row that sees none
     m = -INFINITY;
     l = 0.f;
@@ -1149,13 +1154,44 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
   for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
     for (int r4 = 0; r4 < 4; ++r4) {
-      const int c0 = 32 * cb + 8 * r4 + 4 * half;
       float x[4] = {o[cb][4 * r4], o[cb][4 * r4 + 1], o[cb][4 * r4 + 2], o[cb][4 * r4 + 3]};
       const bool odd = !(fabsf(x[0]) < INFINITY && fabsf(x[1]) < INFINITY && fabsf(x[2]) < INFINITY && fabsf(x[3]) < INFINITY);
-      if (odd && l < INFINITY)
-        sum_values<CT, DH>(a, s, kvh, row, head, max(lo, begin), min(hi, end), m, a.scale * 1.44269504f, c0, x);
-      put_out(a, gr.S, split, (int64_t)s * a.r.max_rows + tok, row, head, DH, c0, m, l, x);
+      if (odd && l < INFINITY) {
+        sum_values<CT, DH>(a, s, kvh, row, head, max(lo, begin), min(hi, end), m, a.scale * 1.44269504f, 32 * cb + 8 * r4 + 4 * half, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[cb][4 * r4 + i] = x[i];
+      }
     }
+  // A lane holds 4 channels of its row here and there: through LDS they become whole rows,
+  // of which 8 neighbouring channels are stored at a time.
+  const int64_t place = ((int64_t)split * a.c.n_seqs + s) * a.r.max_rows, all = (int64_t)gr.S * a.c.n_seqs * a.r.max_rows * a.H;
+  const float inv = l == 0.f ? 0.f : gr.S == 1 ? 1.0f / l : 1.0f;
+  if (gr.S > 1 && half == 0 && qi < nq) reinterpret_cast<float2*>(a.work + all * DH)[(place + tok) * a.H + head] = make_float2(m, l);
+  __syncthreads();  // the tiles are no longer read
+  float* const ow = reinterpret_cast<float*>(lds) + wave * OUT;
+#pragma unroll
+  for (int c1 = 0; c1 < DH; c1 += CP) {
+#pragma unroll
+    for (int cb = c1 / 32; cb < (c1 + CP) / 32; ++cb)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (l != 0.f) x = make_float4(o[cb][4 * r4] * inv, o[cb][4 * r4 + 1] * inv, o[cb][4 * r4 + 2] * inv, o[cb][4 * r4 + 3] * inv);
+        *reinterpret_cast<float4*>(ow + col * (CP + 4) + 32 * cb - c1 + 8 * r4 + 4 * half) = x;
+      }
+    __builtin_amdgcn_wave_barrier();
+    constexpr int PR = CP / 8, RS = 64 / PR;  // lanes of a row, rows at a time
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += RS) {
+      const int r = r0 + lane / PR, c = (lane % PR) * 8, tok2 = __shfl(tok, r), head2 = __shfl(head, r);
+      const float4 x0 = *reinterpret_cast<const float4*>(ow + r * (CP + 4) + c), x1 = *reinterpret_cast<const float4*>(ow + r * (CP + 4) + c + 4);
+      const float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+      if (tile * 128 + wave * 32 + r >= nq) continue;
+      if (gr.S == 1) store_n(a.o.p, (int64_t)(sr.row0 + tok2) * a.o.row + (int64_t)head2 * a.o.head + c1 + c, QT, a.o.vec, x);
+      else store_n(a.work, ((place + tok2) * a.H + head2) * DH + c1 + c, PT_F32, 1, x);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
 // Joins the splits' sums, W waves per (row, head): lane i of each looks after split i's
