@@ -1194,14 +1194,57 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
   }
 }
 
-// Joins the splits' sums, W waves per (row, head): lane i of each looks after split i's
+// Joins up to 8 splits' sums: DH / 4 lanes per (row, head), 4 channels each.
+constexpr int kFewSplits = 8;
+template <int DH>
+__global__ __launch_bounds__(256) void paged_join_few_kernel(PagedAttend a, int S) {
+  constexpr int LR = DH / 4;
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LR;  // place of the row times heads, plus head
+  const int64_t rows = (int64_t)a.c.n_seqs * a.r.max_rows * a.H;
+  if (at >= rows) return;
+  const int c0 = ((int)threadIdx.x & (LR - 1)) * 4;
+  // everything that the sums take is loaded at once; rows that do not exist read what the
+  // workspace holds, and write nothing
+  const float2* ml = reinterpret_cast<const float2*>(a.work + rows * S * DH);
+  float2 st[kFewSplits];
+  float4 p[kFewSplits];
+#pragma unroll
+  for (int k = 0; k < kFewSplits; ++k) {
+    if (k >= S) break;
+    st[k] = ml[k * rows + at];
+    p[k] = *reinterpret_cast<const float4*>(a.work + (k * rows + at) * DH + c0);
+  }
+  const int h = (int)(at % a.H), tok = (int)(at / a.H % a.r.max_rows), s = (int)(at / a.H / a.r.max_rows);
+  const SeqRows sr = seq_rows(a.r, s);
+  if (tok >= sr.n) return;
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int k = 0; k < kFewSplits; ++k) {
+    if (k >= S) break;
+    m = fmaxf(m, st[k].x);
+  }
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int k = 0; k < kFewSplits; ++k) {
+    if (k >= S) break;
+    if (st[k].x == -INFINITY && st[k].y == 0.f) continue;  // saw nothing: may hold anything
+    const float w = __builtin_amdgcn_exp2f(st[k].x - m);
+    l += w * st[k].y;
+    o.x += w * p[k].x; o.y += w * p[k].y; o.z += w * p[k].z; o.w += w * p[k].w;
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  const float x[4] = {l == 0.f ? 0.f : o.x * inv, l == 0.f ? 0.f : o.y * inv, l == 0.f ? 0.f : o.z * inv, l == 0.f ? 0.f : o.w * inv};
+  store_n(a.o.p, (int64_t)(sr.row0 + tok) * a.o.row + (int64_t)h * a.o.head + c0, a.o.type, a.o.vec, x);
+}
+
+// Joins more splits' sums, four waves per (row, head): lane i of each looks after split i's
 // state; a wave's lanes take 4 channels each of 256 / DH splits at a time.
-template <int DH, int W>
+template <int DH>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttend a, int S) {
   constexpr int LR = DH / 4, P = 64 / LR;  // lanes of a split's row, splits at a time
-  __shared__ float4 part[W == 1 ? 1 : 4][LR];
+  __shared__ float4 part[4][LR];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t at = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;  // place of the row times heads, plus head
+  const int64_t at = blockIdx.x;  // place of the row times heads, plus head
   const int64_t rows = (int64_t)a.c.n_seqs * a.r.max_rows * a.H;
   if (at >= rows) return;
   // everything that the sums take is loaded at once; rows that do not exist read what the
@@ -1209,8 +1252,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttend a, int S) {
   const float2* ml = reinterpret_cast<const float2*>(a.work + rows * S * DH);
   float2 st = ml[min(lane, S - 1) * rows + at];
   if (lane >= S) st = make_float2(-INFINITY, 0.f);
-  const int c0 = (lane & (LR - 1)) * 4, first = (W == 1 ? 0 : wave * P) + lane / LR;
-  constexpr int STEP = (W == 1 ? 1 : 4) * P, AHEAD = 4;
+  const int c0 = (lane & (LR - 1)) * 4, first = wave * P + lane / LR;
+  constexpr int STEP = 4 * P, AHEAD = 4;
   float4 p[AHEAD];
 #pragma unroll
   for (int j = 0; j < AHEAD; ++j)
@@ -1236,20 +1279,18 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttend a, int S) {
     }
   }
   o.x = across_sum<LR>(o.x); o.y = across_sum<LR>(o.y); o.z = across_sum<LR>(o.z); o.w = across_sum<LR>(o.w);
-  if constexpr (W > 1) {
-    if (lane < LR) part[wave][lane] = o;
-    __syncthreads();
-    if (wave > 0) return;
-    o = part[0][lane & (LR - 1)];
+  if (lane < LR) part[wave][lane] = o;
+  __syncthreads();
+  if (wave > 0) return;
+  o = part[0][lane & (LR - 1)];
 #pragma unroll
-    for (int k = 1; k < 4; ++k) {
-      const float4 p = part[k][lane & (LR - 1)];
-      o.x += p.x; o.y += p.y; o.z += p.z; o.w += p.w;
-    }
+  for (int k = 1; k < 4; ++k) {
+    const float4 p4 = part[k][lane & (LR - 1)];
+    o.x += p4.x; o.y += p4.y; o.z += p4.z; o.w += p4.w;
   }
   if (lane >= LR) return;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const float x[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+  const float x[4] = {l == 0.f ? 0.f : o.x * inv, l == 0.f ? 0.f : o.y * inv, l == 0.f ? 0.f : o.z * inv, l == 0.f ? 0.f : o.w * inv};
   store_n(a.o.p, (int64_t)(sr.row0 + tok) * a.o.row + (int64_t)h * a.o.head + c0, a.o.type, a.o.vec, x);
 }
 
@@ -1305,10 +1346,10 @@ hipError_t attend_at(const PagedAttend& a, const Plan& p, hipStream_t st, const 
   if (p.step) e = plaunch(paged_step_kernel<CT, DH, QT>, grid, dim3(256), st, ev.start, join ? nullptr : ev.stop, a, p.g);
   else e = plaunch(paged_prompt_kernel<CT, DH, QT>, grid, dim3(256), st, ev.start, join ? nullptr : ev.stop, a, p.g);
   if (e != hipSuccess || !join) return e;
-  const int64_t waves = (int64_t)a.c.n_seqs * a.r.max_rows * a.H;
-  if (p.g.S <= 256 / DH * 4)
-    return plaunch(paged_join_kernel<DH, 1>, dim3((uint32_t)((waves + 3) / 4)), dim3(256), st, nullptr, ev.stop, a, p.g.S);
-  return plaunch(paged_join_kernel<DH, 4>, dim3((uint32_t)waves), dim3(256), st, nullptr, ev.stop, a, p.g.S);
+  const int64_t sums = (int64_t)a.c.n_seqs * a.r.max_rows * a.H;
+  if (p.g.S <= kFewSplits)
+    return plaunch(paged_join_few_kernel<DH>, dim3((uint32_t)((sums * (DH / 4) + 255) / 256)), dim3(256), st, nullptr, ev.stop, a, p.g.S);
+  return plaunch(paged_join_kernel<DH>, dim3((uint32_t)sums), dim3(256), st, nullptr, ev.stop, a, p.g.S);
 }
 
 template <int CT, int DH>
