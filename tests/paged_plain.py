@@ -85,4 +85,5 @@ def attend_bound(terms, out, cache, qt, d, prompt):
     one = same
     dp = (2.0**-11 if one else 2.0**-22) if f16 else (2.0**-8 if one else 2.0**-16)
     lost = 2.0**-24 * av if f16 else 0.0  # probabilities below float16's range
-    return pv * (2 * ds + dp + 2.0**-21 + (seen + 64) * 2.0**-24) + lost + np.abs(out) * HALF_STEP[qt] * 1.01 + 1e-37
+    least = 2.0**-25 if qt == "f16" else 1e-37  # half of the smallest step that the output's type has
+    return pv * (2 * ds + dp + 2.0**-21 + (seen + 64) * 2.0**-24) + lost + np.abs(out) * HALF_STEP[qt] * 1.01 + least

@@ -378,6 +378,29 @@ def test_attend_extreme_scores():
                 c.check([w], 2, "f32", q=q * size, scale=scale)
 
 
+@pytest.mark.parametrize("w", [3, 90])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("ks,vs", [(1e-13, 1.0), (3e12, 1.0), (1.0, 9e3), (1.0, 1e-9), (1e-13, 9e3)])
+def test_attend_scales_beyond_float16(w, d, ks, vs):
+    """Keys and values of four bits whose scales float16 does not hold, in some tiles of a
+    context and not in others, under float16 queries."""
+    import paper_2608_15454_amd as m
+
+    c = Case("mxfp4", [300], 2, d, 16)
+    part = m.PagedRows(ints([0, 100]), ints([90]), 100, 100, 300)
+    k, v = c.k[90:190] * ks, c.v[90:190] * vs
+    c.cache.append(part, k, v)
+    for i, x in ((0, k), (1, v)):
+        c.held[0][i][90:190] = plain.to_mxfp4(f64(x))
+    q = (torch.randn(w, 4, d, generator=c.g, device="cuda")).half()
+    for scale in (1 / np.sqrt(d), 1 / np.sqrt(d) / ks):
+        big = ks > 1 if scale * ks * np.sqrt(d) > 2 else False
+        if not big and scale < 1e6:  # scores of a usable size in the part, or outside it
+            c.check([w], 4, "f16", q=q, scale=scale)
+        lo, hi = np.full(w, 95), np.full(w, 185)  # the part alone
+        c.check([w], 4, "f16", lo=lo, hi=hi, q=q, scale=1 / np.sqrt(d) / ks)
+
+
 def test_attend_strides_alignment_and_given_out():
     d, w = 64, 6
     for kind, qt in (("f16", "f32"), ("bf16", "bf16")):
