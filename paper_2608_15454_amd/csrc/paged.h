@@ -72,4 +72,7 @@ hipError_t launch_paged_read(const PagedCache& c, const PagedRows& r, const Head
                              hipStream_t st, const Ev& ev = Ev());
 hipError_t launch_paged_attend(const PagedAttend& a, hipStream_t st, const Ev& ev = Ev());
 
+// p[i] = i: page tables whose rows' pages lie in order.
+hipError_t launch_paged_iota(int32_t* p, int64_t n, hipStream_t st);
+
 }  // namespace mbp

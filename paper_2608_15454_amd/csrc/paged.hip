@@ -1381,6 +1381,16 @@ size_t paged_work_bytes(const PagedCache& c, const PagedRows& r, int H) {
   return p.g.S > 1 ? (size_t)p.g.S * c.n_seqs * r.max_rows * H * (c.dh + 2) * 4 : 0;
 }
 
+__global__ void paged_iota_kernel(int32_t* p, int64_t n) {
+  const int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
+  if (i < n) p[i] = (int32_t)i;
+}
+
+hipError_t launch_paged_iota(int32_t* p, int64_t n, hipStream_t st) {
+  if (n <= 0) return hipSuccess;
+  return plaunch(paged_iota_kernel, dim3((uint32_t)((n + 255) / 256)), dim3(256), st, nullptr, nullptr, p, n);
+}
+
 // A split launch has at most so many blocks, of 16 or 128 packed rows each.
 size_t paged_work_most(int dh) {
   return (size_t)std::max(16 * kStepBlocks, 128 * kPromptBlocks) * (dh + 2) * 4;

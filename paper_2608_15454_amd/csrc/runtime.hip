@@ -1691,15 +1691,9 @@ extern "C" int mbp_init(const mbp_config* cfg, const void* const* d_weights, int
   h->kv_mb = kvof(rg.mb_k, rg.mb_v, s.Wcap);
   if (s.fp4) {
     // every row's pages in order
-    std::vector<int32_t> up(std::max({(size_t)s.B * s.Tpages, (size_t)s.B * s.Kpages, (size_t)s.Ml}));
-    for (size_t i = 0; i < up.size(); ++i) up[i] = (int32_t)i;
-    auto put = [&](size_t off, size_t n) {
-      if (e == hipSuccess) e = hipMemcpyAsync(h->ws + off, up.data(), n * 4, hipMemcpyHostToDevice, h->st);
-    };
-    put(rg.pages_t, (size_t)s.B * s.Tpages);
-    put(rg.pages_k, (size_t)s.B * s.Kpages);
-    put(rg.iota, (size_t)s.Ml);
-    if (e == hipSuccess) e = hipStreamSynchronize(h->st);
+    e = launch_paged_iota(h->R<int32_t>(rg.pages_t), (int64_t)s.B * s.Tpages, h->st);
+    if (e == hipSuccess) e = launch_paged_iota(h->R<int32_t>(rg.pages_k), (int64_t)s.B * s.Kpages, h->st);
+    if (e == hipSuccess) e = launch_paged_iota(h->R<int32_t>(rg.iota), s.Ml, h->st);
     if (e != hipSuccess) return bail();
     auto paged = [&](KV& k, size_t table, int pages) {
       k.pages = h->R<int32_t>(table);

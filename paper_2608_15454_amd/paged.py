@@ -158,6 +158,8 @@ class PagedCache:
             raise ValueError(f"{name}: [{n_rows}, {'heads' if heads is None else heads}, {self.d_head}] is needed, got {list(shape)}")
         if t.get_device() != self._index:
             raise ValueError(f"{name} is on {t.device}, the cache on {self.device}")
+        if t.requires_grad and self.torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient: these operators have none (detach it, or use no_grad)")
         rs, hs, es = t.stride()
         if es != 1:
             raise ValueError(f"{name}: the channels of a head must be adjacent")

@@ -573,6 +573,42 @@ def test_other_streams():
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("kind,d,page", [("f16", 64, 1024), ("mxfp4", 32, 16), ("bf16", 128, 32)])
+def test_many_sequences(kind, d, page):
+    """More sequences than a wave looks through at once, many of them without rows, at both
+    ends too."""
+    rng = np.random.default_rng(5)
+    lens = [int(n) for n in rng.integers(3, 40, 170)]
+    c = Case(kind, lens, 2, d, page)
+    news = [int(n) for n in rng.integers(0, 4, 170)]
+    news[:70] = [0] * 70
+    news[-3:] = [0, 0, 0]
+    c.check(news, 4, "f32")
+    rows = c.rows(news)
+    k, v = (torch.randn(rows.n_rows, 2, d, generator=c.g, device="cuda") for _ in range(2))
+    c.cache.append(rows, k, v)
+    got = c.cache.read(rows)
+    for x, y in zip((k, v), got):
+        want = plain.to_mxfp4(f64(x)) if kind == "mxfp4" else f64(x.to(TORCH[kind]))
+        assert np.array_equal(f64(y), want)
+
+
+def test_whole_cache_without_sequences_or_rows():
+    import paper_2608_15454_amd as m
+
+    cache = m.PagedCache(m.F16, 2, 64, 16, pages=torch.zeros((0, 4), dtype=torch.int32, device="cuda"), n_pages=3)
+    none = m.PagedRows(ints([0]), ints([]), 5, 5, 5)
+    q = torch.ones(5, 4, 64, device="cuda")
+    assert (cache.attend(none, q) == 0).all() and (cache.read(none)[0] == 0).all()
+    cache.append(none, q[:, :2], q[:, :2])
+    c = Case("f16", [20], 2, 64, 16)
+    empty = m.PagedRows(ints([0, 0]), ints([20]), 0, 0, 20)
+    z = torch.zeros((0, 4, 64), device="cuda")
+    assert c.cache.attend(empty, z).shape == (0, 4, 64)
+    c.cache.append(empty, z[:, :2], z[:, :2], q=z, q_out=torch.zeros_like(z))
+    assert c.cache.read(empty)[1].shape == (0, 2, 64)
+
+
 def test_sequences_share_a_prefix():
     """Two sequences whose first pages are the same."""
     import paper_2608_15454_amd as m
@@ -599,7 +635,7 @@ def test_refusals_of_the_binding():
     r = c.rows([3])
     q, k = torch.zeros(3, 4, 64, device="cuda"), torch.zeros(3, 2, 64, device="cuda")
     bad = [lambda: c.cache.attend(r, q[:2]), lambda: c.cache.attend(r, q[..., :32]), lambda: c.cache.attend(r, q.cpu()),
-           lambda: c.cache.attend(r, q.double()), lambda: c.cache.attend(r, q, out=q.half().double()), lambda: c.cache.attend(r, q.transpose(1, 2)),
+           lambda: c.cache.attend(r, q.double()), lambda: c.cache.attend(r, q.clone().requires_grad_()), lambda: c.cache.attend(r, q, out=q.half().double()), lambda: c.cache.attend(r, q.transpose(1, 2)),
            lambda: c.cache.attend(r, q, lo=torch.zeros(3, device="cuda")), lambda: c.cache.attend(r, q, hi=ints([1, 2])),
            lambda: c.cache.attend(r, q, hi=torch.zeros(3, dtype=torch.int32)), lambda: c.cache.append(r, q, k),
            lambda: c.cache.append(r, k, k, q_out=q), lambda: c.cache.append(r, k, k, rope=torch.zeros(5, 16, 2, device="cuda")),
