@@ -419,15 +419,15 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedCache c, PagedRows
 // cache, bfloat16 for the others (an e2m1 code times a power of two is a bfloat16 value).
 // Queries and probabilities enter as one to three terms of that type, so that what they
 // lose stays below the rounding of the output: kQ query terms, kP probability terms.
-template <int CT, int QT, int MAXQ = 3>
+template <int CT, int QT>
 struct Terms {
   static constexpr bool same = QT == CT || (CT == PT_MXFP4 && QT == PT_BF16);
   // float32 queries: float16 pairs hold 22 bits of a row scaled to its largest value,
   // bfloat16 triples 24; float16 queries over MXFP4 are exact as bfloat16 pairs
-  static constexpr int kQ = same ? 1 : CT == PT_F16 ? 2 : QT == PT_F16 ? 2 : MAXQ;
-  // probabilities: one term has half a step of the output's own type (of bfloat16 for
-  // MXFP4), two terms 2^-16 to 2^-22
-  static constexpr int kP = QT == PT_F32 ? 2 : same ? 1 : 2;
+  static constexpr int kQ = same ? 1 : CT == PT_F16 || QT == PT_F16 ? 2 : 3;
+  // probabilities: one term has half a step of the output's own type, float16 pairs 2^-22;
+  // in bfloat16, a pair (2^-16) for float16 outputs and a triple (2^-24) for float32 ones
+  static constexpr int kP = same ? 1 : CT == PT_F16 || QT == PT_F16 ? 2 : 3;
 };
 
 template <int CT>
@@ -586,7 +586,7 @@ __device__ __forceinline__ void put_out(const PagedAttend& a, int S, int split, 
 // Waves per SIMD that a step kernel's registers leave room for without spills.
 constexpr int step_waves(int ct, int dh, int qt) {
   if (dh < 128) return 4;
-  return ct != PT_MXFP4 ? 2 : qt == PT_BF16 ? 4 : 3;
+  return ct != PT_MXFP4 || qt == PT_F32 ? 2 : qt == PT_BF16 ? 4 : 3;
 }
 
 // Up to 16 query rows of one sequence and KV head (its rows times the query heads of the
@@ -886,7 +886,7 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
 // everything transposed and the values read turned round, as for few rows.
 template <int CT, int DH, int QT>
 __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Grid gr) {
-  using T = Terms<CT, QT, DH == 128 ? 2 : 3>;
+  using T = Terms<CT, QT>;
   constexpr bool F4 = CT == PT_MXFP4;
   // 64 slots a tile, 32 where two terms of 128 channels fill the registers
   constexpr int KT = DH == 128 && T::kQ > 1 ? 32 : 64, NB = KT / 32, NG = KT / 16, KS = DH / 16, CB = DH / 32;

@@ -65,13 +65,13 @@ def attend(q, k, v, lo, hi, scale, have=None):
     return out, (pv, rel, ab, top, seen, av)
 
 
-def attend_bound(terms, out, cache, qt, d, prompt):
+def attend_bound(terms, out, cache, qt, d):
     """Elementwise bound on an attention output's error.  A score is off by what its query
     terms lose (float16 pairs hold a row scaled to its largest value to 2^-22 of it,
     bfloat16 terms 2^-8 of the rest each, equal types nothing) plus the float32 sum over
     the channels and the rounding of the exponent's argument; a probability's relative
     error is twice the largest score error (its own and the sum's), plus the rounding of
-    its one or two 16-bit terms and of exp2 (2^-22); the sum over n slots adds n 2^-24."""
+    its one to three 16-bit terms and of exp2 (2^-22); the sum over n slots adds n 2^-24."""
     pv, rel, ab, top, seen, av = terms
     same = qt == cache or (cache == "mxfp4" and qt == "bf16")
     f16 = cache == "f16"
@@ -80,10 +80,10 @@ def attend_bound(terms, out, cache, qt, d, prompt):
     elif f16:
         dq = 2.0**-22 * ab
     else:
-        dq = (2.0**-16 if prompt and d == 128 else 2.0**-24) * rel
+        dq = 2.0**-24 * rel
     ds = dq + (d + 4) * 2.0**-24 * rel + 16 * 2.0**-24 * top
     one = same
-    dp = (2.0**-11 if one else 2.0**-22) if f16 else (2.0**-8 if one else 2.0**-16)
+    dp = (2.0**-11 if one else 2.0**-22) if f16 else (2.0**-8 if one else 2.0**-16 if qt == "f16" else 2.0**-24)
     lost = 2.0**-24 * av if f16 else 0.0  # probabilities below float16's range
     least = 2.0**-25 if qt == "f16" else 1e-37  # half of the smallest step that the output's type has
     return pv * (2 * ds + dp + 2.0**-21 + (seen + 64) * 2.0**-24) + lost + np.abs(out) * HALF_STEP[qt] * 1.01 + least

@@ -86,7 +86,7 @@ class Case:
             h_ = f0 + np.arange(w) + 1 if hi is None else np.asarray(hi[at:at + w])
             qq = f64(q[at:at + w])
             want, terms = plain.attend(qq, *self.held[i], l_, h_, scale, None if have is None else have[i])
-            tol = plain.attend_bound(terms, want, self.kind, qt, self.d, max(news) * heads // self.hk > 32)
+            tol = plain.attend_bound(terms, want, self.kind, qt, self.d)
             err = np.abs(res[at:at + w] - want)
             assert np.isfinite(res[at:at + w]).all(), f"sequence {i}: not finite"
             assert (err <= tol).all(), f"sequence {i}: off by {err.max():.3g}, {(err / tol).max():.3g} of the bound"
@@ -475,7 +475,7 @@ def test_pools_beyond_four_gibibytes():
         q = torch.randn(w, hk, d, device="cuda")
         got = f64(cache.attend(m.PagedRows(ints([0, w]), ints([n - w]), w, w, n), q))
         want, terms = plain.attend(f64(q[-1:]), f64(k), f64(v), [0], [n], 1 / np.sqrt(d))
-        assert (np.abs(got[-1:] - want) <= plain.attend_bound(terms, want, "bf16", "f32", d, w > 32)).all()
+        assert (np.abs(got[-1:] - want) <= plain.attend_bound(terms, want, "bf16", "f32", d)).all()
     del cache, k, v, gk, gv
     torch.cuda.empty_cache()
 
@@ -550,7 +550,7 @@ def test_prompt_then_steps_in_a_captured_graph():
                 if news[i]:
                     back = cache.read(m.PagedRows(ints([0] * (i + 1) + [every] * (3 - i)), ints([0, 0, 0]), every, every, every))
                     want, terms = plain.attend(f64(q2[r:r + news[i]]), *(f64(b) for b in back), np.zeros(news[i]), at[i] + 1 + np.arange(news[i]), 1 / np.sqrt(d))
-                    tol = plain.attend_bound(terms, want, kind, "f32", d, False)
+                    tol = plain.attend_bound(terms, want, kind, "f32", d)
                     assert (np.abs(f64(out[r:r + news[i]]) - want) <= tol).all()
                 r += news[i]
                 at[i] = every
@@ -625,7 +625,7 @@ def test_sequences_share_a_prefix():
     for i in range(2):
         kk, vv = (f64(torch.cat([x, ends[i:i + 1]]).half()) for x in (k, v))
         want, terms = plain.attend(f64(q[i:i + 1]), kk, vv, [0], [33], 1 / np.sqrt(d))
-        assert (np.abs(got[i:i + 1] - want) <= plain.attend_bound(terms, want, "f16", "f32", d, False)).all()
+        assert (np.abs(got[i:i + 1] - want) <= plain.attend_bound(terms, want, "f16", "f32", d)).all()
 
 
 def test_refusals_of_the_binding():
