@@ -601,6 +601,9 @@ constexpr int step_waves(int ct, int dh, int qt) {
 //   O^T += V^T P^T: the probabilities are already where the product wants them, values
 //     go through the wave's own LDS tile and are read turned round.
 // The next block's loads are in flight during a block's softmax and value product.
+// Bound by the cache's stream: 5.4 TB/s over 64 float16 sequences of 1024 to 2048 slots, 5.8
+// over 16 bfloat16 ones of 8192 (a large copy: 4.7); over MXFP4 by the instructions of
+// decoding and softmax, 3.5 TB/s with float32 rows of d = 64, 4.9 with bfloat16 rows of d = 128.
 template <int CT, int DH, int QT>
 __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel(PagedAttend a, Grid gr) {
   using T = Terms<CT, QT>;
@@ -883,7 +886,10 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
 // LDS for all four waves, the next 64 are loaded during the products.  32x32x16 products
 // (lane l supplies row or column l % 32 and the 8 positions 8 (l / 32).. of the
 // contracted dimension, and receives rows 8 (r / 4) + 4 (l / 32) + r % 4 of column l % 32);
-// everything transposed and the values read turned round, as for few rows.
+// everything transposed and the values read turned round, as for few rows.  The matrix cores
+// and the softmax's vector instructions share the time: causal prompts of 4 x 4096 rows and
+// 32 heads over 8 run at 845 TFLOP/s (d = 128, bfloat16), 912 (MXFP4) and 775 (d = 64), where
+// a library product reaches 1235.
 template <int CT, int DH, int QT>
 __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Grid gr) {
   using T = Terms<CT, QT>;
@@ -1294,9 +1300,15 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttend a, int S) {
   store_n(a.o.p, (int64_t)(sr.row0 + tok) * a.o.row + (int64_t)h * a.o.head + c0, a.o.type, a.o.vec, x);
 }
 
-// Few packed rows (rows of a sequence times query heads of a KV head) run on the step
-// kernel.
-constexpr int kStepRows = 32;
+// Packed rows (rows of a sequence times query heads of a KV head) up to which the step
+// kernel runs.  It reads the cache once for every 16 rows, the prompt kernel once for 128 but
+// in tiles whose loads and products a block does in turn.  us in a graph, step and prompt:
+// float16 d = 64, one sequence of 4096 slots, 32 rows 10.9 and 13.6, 33 rows 15.0 and 14.1;
+// 16 of 2048, 16 rows 25.7 and 36.3, 32 rows 43 and 38, 64 rows 77 and 46; bfloat16 d = 128,
+// 4 of 4096, 32 rows 18.9 and 23.4, 36 rows 34 and 24.  Over MXFP4, where reading again costs
+// a quarter: d = 128, 4 of 8192, 32 rows 19 and 35, 128 rows 40 and 49; float32 rows, d = 64,
+// 16 of 2048, 33 rows 28 and 46, 128 rows 63 and 63.
+constexpr int step_rows(int type) { return type == PT_MXFP4 ? 128 : 32; }
 constexpr int kMaxSplits = 64;
 // blocks of a launch up to which the slots are split
 constexpr int kStepBlocks = 1024, kPromptBlocks = 1024;
@@ -1321,7 +1333,7 @@ Plan plan_of(const PagedCache& c, const PagedRows& r, int H) {
   Plan p;
   p.g.G = H / c.hk;
   const int64_t packed = (int64_t)r.max_rows * p.g.G;
-  p.step = packed <= kStepRows;
+  p.step = packed <= step_rows(c.type);
   const int64_t per = p.step ? 16 : 128;
   p.g.tiles = (int)((packed + per - 1) / per);
   const int64_t blocks = std::max<int64_t>((int64_t)p.g.tiles * c.n_seqs * c.hk, 1), slots = std::max(r.max_slots, 1);
