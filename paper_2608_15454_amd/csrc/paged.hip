@@ -446,12 +446,13 @@ __device__ __forceinline__ float hi_of(uint32_t u) {
   else return hi_bf16(u);
 }
 
-// 8 values as N terms of the product's type, each the rounded rest of the ones before.
+// 8 values, times a power of two, as N terms of the product's type, each the rounded rest of
+// the ones before.
 template <int CT, int N>
-__device__ __forceinline__ void split8(const float (&x)[8], u32x4 (&t)[N]) {
+__device__ __forceinline__ void split8(const float (&x)[8], u32x4 (&t)[N], float gain = 1.f) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float a = x[2 * i], b = x[2 * i + 1];
+    float a = x[2 * i] * gain, b = x[2 * i + 1] * gain;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const uint32_t u = pack_pair<CT>(a, b);
@@ -562,9 +563,13 @@ struct Grid {  // of an attention launch: x is split fastest, then tile; y the K
 
 // Probabilities are 2^(f s - f m) with a reference m that need not be the largest score:
 // it follows once one is more than 2^kSlack times as probable, so that the sums are
-// rescaled a few times in a row's life instead of at every block.  2^8 keeps float16
-// terms far from the type's ends.
+// rescaled a few times in a row's life instead of at every block.  Float16 terms, and the
+// value sums until the end, are kGain times larger: at most 2^15, within the type, whose
+// smallest step is then 2^-31 of a probability of 1 (without it a million slots of 2^-25
+// each, a thirtieth of the sum, would be left out).
 constexpr float kSlack = 8.f;
+template <int CT>
+constexpr float kGain = CT == PT_F16 ? 128.f : 1.f;
 
 // Where a row's channels go: the output, or this split's sums, at place `place` (its
 // sequence's place times max_rows, plus the row's in that: known without a load).
@@ -818,7 +823,7 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
     for (int b = 0; b < NB; b += 2) {
       const float y[8] = {sc[b][0], sc[b][1], sc[b][2], sc[b][3], sc[b + 1][0], sc[b + 1][1], sc[b + 1][2], sc[b + 1][3]};
       u32x4 p[T::kP];
-      split8<CT, T::kP>(y, p);
+      split8<CT, T::kP>(y, p, kGain<CT>);
       const uint16_t* src = vt + (16 * b + 4 * g + (col >> 2)) * PITCH + (col & 3) * 4;
       u32x4 vf[CB];
 #pragma unroll
@@ -834,6 +839,8 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
     __builtin_amdgcn_wave_barrier();
   }
   l = across_sum<16>(l);
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) o[cb] *= 1 / kGain<CT>;
   if (hi == 0) {  // blocks that all other rows see whole were not masked for a row that sees none
     m = -INFINITY;
     l = 0.f;
@@ -1132,7 +1139,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
           const float x[8] = {sc[b][8 * k2], sc[b][8 * k2 + 1], sc[b][8 * k2 + 2], sc[b][8 * k2 + 3],
                               sc[b][8 * k2 + 4], sc[b][8 * k2 + 5], sc[b][8 * k2 + 6], sc[b][8 * k2 + 7]};
           u32x4 p[T::kP];
-          split8<CT, T::kP>(x, p);
+          split8<CT, T::kP>(x, p, kGain<CT>);
           // lanes of a quarter wave: channels 16 (lane / 16 % 2) .., slots 4 half .. of the 8
           const uint16_t* src = vt + (32 * b + 16 * k2 + 4 * half + ((lane & 15) >> 2)) * VP + (lane & 16) + (lane & 3) * 4;
           u32x4 vf[CB];
@@ -1151,6 +1158,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
     if (more) store(t + KT, cur ^ 1);
   }
   l = pair_sum<32>(l);
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) o[cb] *= 1 / kGain<CT>;
   if (hi == 0) {  // tiles that all other rows see whole were not masked for a row that sees none
     m = -INFINITY;
     l = 0.f;

@@ -653,3 +653,24 @@ def test_refusals_of_the_binding():
         with pytest.raises(m.MbpError) as e:
             f()
         assert e.value.code == m.EINVAL and str(e.value)
+
+
+@pytest.mark.parametrize("qt", ["f32", "f16"])
+@pytest.mark.parametrize("w", [1, 200])
+def test_attend_many_improbable_slots(qt, w):
+    """Slots 2^24.7 times less probable than the largest, below float16's smallest step, still
+    count: 31 of them, worth 1000 each, beside every one that is probable and worth 0."""
+    import paper_2608_15454_amd as m
+
+    n, d = 480, 64
+    cache = m.PagedCache(m.F16, 1, d, 32, pages=ints([list(range(16))]), n_pages=16)
+    k, v = torch.zeros(n, 1, d, device="cuda"), torch.full((n, 1, d), 1000.0, device="cuda")
+    k[::32], v[::32] = 2.14, 0.0
+    cache.append(m.PagedRows(ints([0, n]), ints([0]), n, n, n), k, v)
+    q = torch.ones(w, 1, d, device="cuda", dtype=TORCH[qt])
+    got = f64(cache.attend(m.PagedRows(ints([0, w]), ints([0]), w, w, n), q, hi=ints([n] * w)))
+    want = 31 * 1000.0 / (np.exp(8 * float(np.float16(2.14))) + 31)
+    # a term of an improbable slot is off by at most half of float16's smallest step, 2^-25, of
+    # values held 2^7 times larger beside a largest one of at least 2^-0.5; a score's float32
+    # sum and exponent by far less than 2^-10, the output's rounding likewise
+    assert np.abs(got - want).max() <= 31 * 1000 * 2.0**-31.5 + 2.0**-10 * want
