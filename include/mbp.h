@@ -452,7 +452,7 @@ size_t mbp_paged_workspace_bytes(const mbp_paged_cache *cache, const mbp_paged_r
  *               cache's own 16-bit dtype, or either over MBP_MXFP4.
  *   d_lo, d_hi  int32 [n_rows]: the slots that each row sees, for causal, document, group,
  *               prefix and window masks alike.  NULL: from slot 0; up to the row's own.
- *   scale       finite, 1 / sqrt(d_head) as a rule.
+ *   scale       1 / sqrt(d_head) as a rule; of magnitude below 2.3e38.
  *   d_work      device workspace of work_bytes >= mbp_paged_workspace_bytes, aligned to 16
  *               bytes, contents of no matter; used until the call's work has finished.
  * Scores, softmax and sums are float32.  What slots hold that a row does not see, be it

@@ -446,6 +446,14 @@ __device__ __forceinline__ float hi_of(uint32_t u) {
   else return hi_bf16(u);
 }
 
+// The exponent that brings a row whose largest magnitude is top into float16 as x 2^-e; its
+// scores then count 2^e times as much, in a factor kept within float32's normal numbers
+// (beyond them scores either differ by far too much or by nothing).  From 2^113 on the row
+// rather fills float16.
+__device__ __forceinline__ int fit16(float top) {
+  return min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 113);
+}
+
 // 8 values, times a power of two, as N terms of the product's type, each the rounded rest of
 // the ones before.
 template <int CT, int N>
@@ -568,6 +576,7 @@ struct Grid {  // of an attention launch: x is split fastest, then tile; y the K
 // smallest step is then 2^-31 of a probability of 1 (without it a million slots of 2^-25
 // each, a thirtieth of the sum, would be left out).
 constexpr float kSlack = 8.f;
+constexpr float kFar = 1048576.f;  // f m whose rounding, 2^-4, is no more than its scores' own
 template <int CT>
 constexpr float kGain = CT == PT_F16 ? 128.f : 1.f;
 
@@ -734,9 +743,9 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
 #pragma unroll
       for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[ks][i]));
     top = across_max<16>(top);
-    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+    const int e = fit16(top);
     sign = ldexpf(sign, -e);
-    f = ldexpf(f, e);
+    f = fminf(fmaxf(ldexpf(f, e), 0x1p-126f), 0x1.fffffep127f);
   }
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
@@ -802,7 +811,7 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
 #pragma unroll
       for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[b][r]);
     mx = across_max<16>(mx);
-    if (__any(mx * f > fmaf(m, f, kSlack) || m == -INFINITY)) {
+    if (__any((mx - m) * f > kSlack || m == -INFINITY)) {
       const float mn = fmaxf(m, mx);
       const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * f);
       m = mn;
@@ -810,7 +819,16 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) o[cb] *= alpha;
     }
-    const float ref = m == -INFINITY ? 0.f : m * f;
+    float ref = m == -INFINITY ? 0.f : m * f;
+    if (__any(fabsf(ref) > kFar)) {  // the product's rounding would be taken for a score
+      asm volatile("" ::: "memory");
+      const float off = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sc[b][r] -= off;
+      ref = 0.f;
+    }
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -1061,9 +1079,9 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
       for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
     }
     top = pair_max<32>(top);
-    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+    const int e = fit16(top);
     sign = ldexpf(sign, -e);
-    f = ldexpf(f, e);
+    f = fminf(fmaxf(ldexpf(f, e), 0x1p-126f), 0x1.fffffep127f);
   }
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
@@ -1116,7 +1134,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[b][r]);
       mx = pair_max<32>(mx);
-      if (__any(mx * f > fmaf(m, f, kSlack) || m == -INFINITY)) {
+      if (__any((mx - m) * f > kSlack || m == -INFINITY)) {
         const float mn = fmaxf(m, mx);
         const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * f);
         m = mn;
@@ -1124,7 +1142,16 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Gri
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) o[cb] *= alpha;
       }
-      const float ref = m == -INFINITY ? 0.f : m * f;
+      float ref = m == -INFINITY ? 0.f : m * f;
+      if (__any(fabsf(ref) > kFar)) {  // the product's rounding would be taken for a score
+        asm volatile("" ::: "memory");
+        const float off = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sc[b][r] -= off;
+        ref = 0.f;
+      }
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll

@@ -205,7 +205,7 @@ int mbp_paged_attend(const mbp_paged_cache* cache, const mbp_paged_rows* rows, i
   if (q->dtype != MBP_F32 && cache->dtype != MBP_MXFP4 && q->dtype != cache->dtype)
     return refuse(MBP_EINVAL, "q must be MBP_F32 or of the cache's 16-bit dtype");
   if (!aligned(d_lo, 4) || !aligned(d_hi, 4)) return refuse(MBP_EINVAL, "d_lo and d_hi must be aligned to 4 bytes");
-  if (!std::isfinite(scale)) return refuse(MBP_EINVAL, "scale must be finite");
+  if (!std::isfinite(scale * 1.44269504f)) return refuse(MBP_EINVAL, "scale must be finite and below 2.3e38");
   a.H = n_heads;
   a.lo = d_lo;
   a.hi = d_hi;

@@ -674,3 +674,59 @@ def test_attend_many_improbable_slots(qt, w):
     # values held 2^7 times larger beside a largest one of at least 2^-0.5; a score's float32
     # sum and exponent by far less than 2^-10, the output's rounding likewise
     assert np.abs(got - want).max() <= 31 * 1000 * 2.0**-31.5 + 2.0**-10 * want
+
+
+@pytest.mark.parametrize("w", [2, 150])
+def test_attend_queries_and_scales_at_the_ends_of_float32(w):
+    """Float32 queries of zeros under a tiny scale see a mean, huge ones the largest score's
+    value: whatever a row is scaled by on its way into float16 stays a number."""
+    import paper_2608_15454_amd as m
+
+    n, d = 100, 64
+    cache = m.PagedCache(m.F16, 1, d, 32, pages=ints([list(range(4))]), n_pages=4)
+    k, v = torch.zeros(n, 1, d, device="cuda"), torch.randn(n, 1, d, device="cuda").half().float()
+    k[:, 0, 0] = (torch.arange(n, device="cuda") * 37 % n + 1) * 2.0**-10
+    cache.append(m.PagedRows(ints([0, n]), ints([0]), n, n, n), k, v)
+    rows = m.PagedRows(ints([0, w]), ints([0]), w, w, n)
+    lo, hi = ints([5] * w), ints([77] * w)
+    q = torch.zeros(w, 1, d, device="cuda")
+    held = f64(v)[5:77, 0]
+    for scale in (1e-9, 1e-40, 0.125, 2e38):
+        got = f64(cache.attend(rows, q, lo=lo, hi=hi, scale=scale))
+        # 72 equal probabilities: a float32 sum of 72 values of at most 6
+        assert np.abs(got - held.mean(0)).max() <= 6 * 72 * 2.0**-24
+    best = held[np.argmax(np.arange(n)[5:77] * 37 % n)]
+    for size, scale in ((2.0**126, 4.0), (1.5 * 2.0**127, 0.125), (2.0**120, 2.0**10), (2.0**100, 1.0), (2.0**30, 2.0**90)):
+        q[:, :, 0] = size
+        got = f64(cache.attend(rows, q, lo=lo, hi=hi, scale=scale))
+        assert np.abs(got - best).max() <= 6 * 2.0**-22, (size, scale)
+
+
+@pytest.mark.parametrize("w", [2, 150])
+@pytest.mark.parametrize("kind,qt", PAIRS)
+def test_attend_scores_beyond_the_bits_of_float32(kind, qt, w):
+    """Scores so large that float32 holds no fraction of them: the largest takes all, whatever
+    their sign, and equal ones share."""
+    import paper_2608_15454_amd as m
+
+    n, d = 100, 64
+    cache = m.PagedCache(number(kind), 1, d, 32, pages=ints([list(range(4))]), n_pages=4)
+    k, v = torch.zeros(n, 1, d, device="cuda"), torch.randn(n, 1, d, device="cuda")
+    rank = torch.arange(n, device="cuda") * 37 % n
+    # four slots of each power of two: the largest (or smallest) of those seen share everything
+    k[:, 0, 0] = 1.5 * 2.0 ** -(rank // 4)
+    cache.append(m.PagedRows(ints([0, n]), ints([0]), n, n, n), k, v)
+    held = f64(cache.read(m.PagedRows(ints([0, n]), ints([0]), n, n, n))[1])[:, 0]
+    rows = m.PagedRows(ints([0, w]), ints([0]), w, w, n)
+    lo, hi = ints([3] * w), ints([88] * w)
+    at = f64(k)[3:88, 0, 0]
+    q = torch.zeros(w, 1, d, device="cuda", dtype=TORCH[qt])
+    q[:, :, 0] = 1.375
+    for scale in (1e12, 3e7 / 1.1, 7.77e15, -1e25, -3.3e33):
+        got = f64(cache.attend(rows, q, lo=lo, hi=hi, scale=scale))
+        x = scale * 1.375 * at
+        p = np.exp(np.clip(x - x.max(), -700, 0))
+        want = (p[:, None] * held[3:88]).sum(0) / p.sum()
+        # the sharing slots' probabilities are 1: a sum of four values and the output's rounding
+        half = {"f32": 2.0**-24, "f16": 2.0**-11, "bf16": 2.0**-8}[qt]
+        assert np.abs(got - want).max() <= 6 * (2 * half + 2.0**-20), scale

@@ -139,3 +139,7 @@ def test_calls_too_large_for_a_launch(L):
 def test_pool_bytes(L):
     for dtype, slot in ((m.F16, 128), (m.BF16, 128), (m.MXFP4, 34)):
         assert L.mbp_paged_pool_bytes(ref(cache(dtype=dtype))) == 4 * 2 * 16 * slot
+
+
+def test_scales_beyond_float32_in_base_two(L):
+    assert attend(L, scale=2.5e38) == m.EINVAL and attend(L, scale=-2.5e38) == m.EINVAL
