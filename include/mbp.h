@@ -423,7 +423,8 @@ int mbp_rope_table(float *d_table, int32_t n_pos, int32_t d_head, float base, vo
 /* Append token rows: keys are rotated and, like the values, stored in their slots; with
  * queries, those are rotated into q_out.
  *   q, q_out    n_heads heads each (a multiple of n_kv_heads), of one dtype; both NULL for
- *               none (n_heads is not read then).  q_out may be q itself.
+ *               none (n_heads is not read then).  q_out may be q itself and else
+ *               overlaps nothing.
  *   k, v        n_kv_heads heads.
  *   d_pos       int32 [n_rows] rotary positions, or NULL: the rows' slots.
  *   d_rope      table of n_pos positions as mbp_rope_table makes it, or NULL: no rotation
@@ -449,7 +450,8 @@ size_t mbp_paged_workspace_bytes(const mbp_paged_cache *cache, const mbp_paged_r
  *   out[r][h] = sum over s of softmax_s(scale q[r][h] . k[s][h / (n_heads / n_kv_heads)]) v[s][..]
  * over the slots lo <= s < hi that have a page; 0 for a row that sees none.
  *   q, out      n_heads heads (a multiple of n_kv_heads), of one dtype: MBP_F32, the
- *               cache's own 16-bit dtype, or either over MBP_MXFP4.
+ *               cache's own 16-bit dtype, or either over MBP_MXFP4.  out may be q itself
+ *               and else overlaps nothing.
  *   d_lo, d_hi  int32 [n_rows]: the slots that each row sees, for causal, document, group,
  *               prefix and window masks alike.  NULL: from slot 0; up to the row's own.
  *   scale       1 / sqrt(d_head) as a rule; of magnitude below 2.3e38.

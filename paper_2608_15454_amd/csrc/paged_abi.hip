@@ -202,6 +202,8 @@ int mbp_paged_attend(const mbp_paged_cache* cache, const mbp_paged_rows* rows, i
   CK(check_heads("q", q, n_heads, a.r.n_rows, a.c.dh, false, &a.q));
   CK(check_heads("out", out, n_heads, a.r.n_rows, a.c.dh, true, &a.o));
   if (q->dtype != out->dtype) return refuse(MBP_EINVAL, "q and out must have one dtype");
+  if (q->d == out->d && (q->row_stride != out->row_stride || q->head_stride != out->head_stride))
+    return refuse(MBP_EINVAL, "out in the place of q must have its strides");
   if (q->dtype != MBP_F32 && cache->dtype != MBP_MXFP4 && q->dtype != cache->dtype)
     return refuse(MBP_EINVAL, "q must be MBP_F32 or of the cache's 16-bit dtype");
   if (!aligned(d_lo, 4) || !aligned(d_hi, 4)) return refuse(MBP_EINVAL, "d_lo and d_hi must be aligned to 4 bytes");

@@ -227,7 +227,8 @@ class PagedCache:
     def attend(self, rows, q, out=None, lo=None, hi=None, scale=None):
         """Attention of ``q`` [n_rows, heads, d_head] over slots ``lo`` .. ``hi`` - 1 (int32
         [n_rows]; by default 0 and the row's own slot + 1) of each row's sequence.  Rows that
-        belong to no sequence are 0 in an allocated ``out`` and left alone in a given one."""
+        belong to no sequence are 0 in an allocated ``out`` and left alone in a given one,
+        which may be ``q``."""
         self._check_rows(rows)
         n, torch = rows.n_rows, self.torch
         qs = self._heads("q", q, n)

@@ -730,3 +730,13 @@ def test_attend_scores_beyond_the_bits_of_float32(kind, qt, w):
         # the sharing slots' probabilities are 1: a sum of four values and the output's rounding
         half = {"f32": 2.0**-24, "f16": 2.0**-11, "bf16": 2.0**-8}[qt]
         assert np.abs(got - want).max() <= 6 * (2 * half + 2.0**-20), scale
+
+
+@pytest.mark.parametrize("w,n", [(1, 300), (3, 4000), (90, 400), (200, 3000)])
+@pytest.mark.parametrize("kind,qt", [("f16", "f32"), ("bf16", "bf16"), ("mxfp4", "f16")])
+def test_attend_in_place(kind, qt, w, n):
+    c = Case(kind, [n, n // 2], 2, 64, 32)
+    q = torch.randn(2 * w, 6, 64, generator=c.g, device="cuda").to(TORCH[qt])
+    rows = c.rows([w, w])
+    want = c.cache.attend(rows, q)
+    assert c.cache.attend(rows, q, out=q) is q and torch.equal(q, want)

@@ -143,3 +143,8 @@ def test_pool_bytes(L):
 
 def test_scales_beyond_float32_in_base_two(L):
     assert attend(L, scale=2.5e38) == m.EINVAL and attend(L, scale=-2.5e38) == m.EINVAL
+
+
+def test_out_in_the_place_of_q(L):
+    assert attend(L, q=heads(4), out=heads(4, row_stride=999)) == m.EINVAL
+    assert b"place of q" in L.mbp_paged_error()
