@@ -913,7 +913,7 @@ __global__ __launch_bounds__(256, step_waves(CT, DH, QT)) void paged_step_kernel
 // contracted dimension, and receives rows 8 (r / 4) + 4 (l / 32) + r % 4 of column l % 32);
 // everything transposed and the values read turned round, as for few rows.  The matrix cores
 // and the softmax's vector instructions share the time: causal prompts of 4 x 4096 rows and
-// 32 heads over 8 run at 845 TFLOP/s (d = 128, bfloat16), 912 (MXFP4) and 775 (d = 64), where
+// 32 heads over 8 run at 833 TFLOP/s (d = 128, bfloat16), 901 (MXFP4) and 768 (d = 64), where
 // a library product reaches 1235.
 template <int CT, int DH, int QT>
 __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttend a, Grid gr) {
